@@ -57,7 +57,7 @@ enum {
                                8-bit HiF8 result (Algorithm 2); no restart, lambda is ignored */
 };
 
-enum { BAPS_DTYPE_BF16 = 0, BAPS_DTYPE_F32 = 1 };
+enum { BAPS_DTYPE_BF16 = 0, BAPS_DTYPE_F32 = 1, BAPS_DTYPE_F16 = 2 };
 
 typedef struct CUstream_st *baps_stream;
 
@@ -209,6 +209,110 @@ baps_status baps_attention_restart_rates_static(const void *q, const void *k, co
                                                 int B, int H, int Hkv, int S, int D, int causal,
                                                 int block_q, int block_k, int lambda, float *rates,
                                                 baps_stream stream);
+
+/* ==== Serving: prompts and single tokens of models with a sliding window, on an 8-bit cache ===========
+ *
+ * The calls below serve one decoding loop: baps_attention_window_fwd the prompts, baps_kv_append the keys and
+ * values that go into the cache, baps_kv_attention the new tokens, baps_kv_fork and baps_kv_compact the pages.
+ * They compute the plain softmax (Eq. (1)), in single precision around tensor-core products; none of Algorithm 1.
+ *
+ * Visibility.  The query at position p sees key j where j <= p and (j > p - window or j < sinks): itself, the
+ * window - 1 keys before it and the sequence's first `sinks` keys.  window >= 1 (INT32_MAX: all), sinks >= 0.
+ * A key that a row does not see has no influence on it, whatever is stored there -- but for a NaN or infinity in
+ * a row of V that other rows of the same call do see: it can make NaN of rows that share its 128-key tile.  */
+
+/* ---- Windowed attention of whole prompts ----------------------------------------------------------
+ * out[b, h, r] = sum_c softmax_c(scale * q[b, h, r] . k[b, h / (H / Hkv), c]) v[b, h / (H / Hkv), c] over the
+ * visible c < lengths[b], r < lengths[b].  lengths: device int32 [B] (NULL: S everywhere; values are read as
+ * limited to 0..S).  Rows r >= lengths[b] of out and lse are left as they are, and what stands in those rows of
+ * q, k and v does not matter.  lse: NULL or device float [B, H, S], the natural logarithm of the sum of exponentials.
+ * strides: NULL for contiguous [B, heads, S, D], else 12 int64 in elements: batch, head and row of q, k, v and out,
+ * each at least 8 and a multiple of 8; the D elements of a row are contiguous.  Tensors must not overlap out.
+ * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q, k, v and out).  scale: 0 selects 1/sqrt(D).
+ * Supported (else BAPS_ERR_UNSUPPORTED): D in {64, 128}; any S >= 1; H % Hkv == 0; B, H <= 65535.           */
+baps_status baps_attention_window_fwd(const void *q, const void *k, const void *v, void *out, float *lse,
+                                      const int32_t *lengths, const int64_t *strides, int B, int H, int Hkv, int S,
+                                      int D, int window, int sinks, float scale, int dtype, baps_stream stream);
+
+/* ---- The cache ---------------------------------------------------------------------------------------
+ * A pool of pages.  k, v: [n_pages, Hkv, page, D] FP8 E4M3 codes (OCP, as in baps_attention_fwd_fp8); k_scale, v_scale:
+ * [n_pages, Hkv] float32, one power of two per page and head: an element stands for value(code) * scale.  All device memory of
+ * the caller, codes 16-byte and scales 4-byte aligned.  page in {16, 32, 64, 128}, D in {64, 128}.
+ * A sequence's pages are named by its row of a table, int32 [rows, table_width]: token j stands at place j % page of page
+ * table[row][j / page].  An entry outside 0 .. n_pages - 1 (-1 by convention) names no page: nothing is written there,
+ * and its keys are invisible.                                                                          */
+typedef struct {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    int n_pages, Hkv, page, D;
+} baps_kv_cache;
+
+/* ---- New tokens into the cache ------------------------------------------------------------------------
+ * k_new, v_new: tokens of all sequences one after the other, element (i, head, d) at i * stride[0] + head * stride[1] + d
+ * (strides: 4 int64 -- token and head of k_new, then of v_new -- multiples of 8; NULL: contiguous [n_tokens, Hkv, D]).
+ * starts: device int32 [B + 1]: tokens starts[b] .. starts[b + 1] - 1 belong to sequence b (limited to 0 .. n_tokens and to
+ * max_new each).  lengths: device int32 [B], tokens that the sequence holds before the call; the new ones follow.
+ * The caller adds to lengths itself.
+ * Scales: let a be the largest finite magnitude that the call brings to a page and head (at least 2^-100).  The new scale
+ * is the smallest power of two s with a <= 448 s, and not below the old scale where the page holds older tokens of the
+ * sequence; where it grew, all codes of that page and head that the call does not write -- places behind the new tokens
+ * included -- are rounded again: code = E4M3(value(code) * old / new).  A new element becomes E4M3(x / s), to
+ * nearest even, infinities to +-448, NaN to NaN.  A page whose first place is written begins anew.
+ * Two sequences must not write to one page in the same call.  Codes and scales do not depend on how tokens are spread
+ * over calls, but for the second rounding of elements that a grown scale makes subnormal.
+ * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16.                                                             */
+baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const void *v_new, const int64_t *strides,
+                           int64_t n_tokens, const int32_t *starts, const int32_t *lengths, const int32_t *table,
+                           int table_width, int B, int max_new, int dtype, baps_stream stream);
+
+/* ---- Attention of the last T tokens of every sequence over the cache ------------------------------------
+ * q, out: [B, H, T, D]; query t of sequence b stands at position lengths[b] - T + t, keys are those of positions
+ * 0 .. lengths[b] - 1 (lengths: device int32 [B], the new tokens included; read as limited to 0 .. table_width * page).
+ * A row that sees no key (a position below 0, pages that are not there) gives zeros and an lse of -infinity.
+ * Only pages that hold a visible key are read.  lse: NULL or device float [B, H, T].  strides: NULL for contiguous, else
+ * 6 int64 in elements, multiples of 8: batch, head and token of q, then of out.
+ * workspace: device memory, 16-byte aligned, at least baps_kv_attention_workspace() bytes, contents irrelevant before and
+ * after; calls that may run at the same time need one each.
+ * Value scales of a sequence and head that are more than 2^64 apart: the smaller values may count as zero.
+ * Results are the same from call to call.  dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q and out).  scale: 0: 1/sqrt(D).
+ * Supported: T <= 16; H % Hkv == 0; B <= 4096.                                                             */
+baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_kv_cache *cache, const int32_t *table,
+                              int table_width, const int32_t *lengths, const int64_t *strides, int B, int H, int T,
+                              int window, int sinks, float scale, int dtype, void *workspace, size_t workspace_bytes,
+                              baps_stream stream);
+/* Bytes of workspace for these sizes on the current device; 0 for sizes that baps_kv_attention refuses. */
+size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D);
+
+/* ---- Pages: rows of a batch rebuilt from parents --------------------------------------------------------
+ * One step of a serving loop's bookkeeping, without the host knowing a length: new row i of the table becomes a
+ * continuation of old row parents[i] -- forked where a parent is named several times, moved where once, its pages given up
+ * where never, an empty row (length 0) where parents[i] is outside 0 .. rows - 1 -- with room for `reserve` more tokens.
+ *   - Full pages are shared.  The page that a sequence ends in (length % page != 0) goes to the parent's first child;
+ *     every further child gets a copy of it in a free page.
+ *   - Pages whose keys no later query sees (window, sinks as above, the next query at position length) are let go: -1.
+ *   - Behind them come free pages for tokens up to length + reserve.
+ *   - Free pages are those with refs == 0, taken lowest first, row after row (a row's copy before its reserve).  The
+ *     first row that finds too few, and every row behind it, gets length -1 and no pages; so does a row that
+ *     table_width cannot hold (which takes none from the rows behind it).
+ *   - new_refs[p]: number of entries of new_table that name page p.  new_table is -1 elsewhere.
+ * refs, new_refs: device int32 [cache->n_pages]; table [rows, table_width], new_table [new_rows, table_width]; lengths [rows],
+ * new_lengths [new_rows].  In- and outputs must not overlap.  workspace: at least baps_kv_pages_workspace(new_rows, n_pages)
+ * bytes.  cache->k and v are only written for copies.                                                      */
+baps_status baps_kv_fork(const baps_kv_cache *cache, const int32_t *table, const int32_t *lengths, int rows,
+                         const int32_t *refs, const int32_t *parents, int new_rows, int table_width, int reserve,
+                         int window, int sinks, int32_t *new_table, int32_t *new_lengths, int32_t *new_refs,
+                         void *workspace, size_t workspace_bytes, baps_stream stream);
+
+/* ---- Pages: those in use moved to the front of the pool ----------------------------------------------
+ * n = number of pages with refs > 0 (written to n_live).  The k-th used page at or behind n moves to the k-th free page
+ * before n: codes, scales and count; all others stay.  page_map[p]: where page p is now (-1: free);
+ * new_table = page_map of table (-1 stays); new_refs: the counts at their new places, 0 from n on.
+ * Device int32 arrays: table, new_table [rows, table_width] (rows may be 0), refs, new_refs, page_map [n_pages],
+ * n_live [1].  In- and outputs must not overlap.                                                          */
+baps_status baps_kv_compact(const baps_kv_cache *cache, const int32_t *table, int rows, int table_width, const int32_t *refs,
+                            int32_t *new_table, int32_t *new_refs, int32_t *page_map, int32_t *n_live,
+                            void *workspace, size_t workspace_bytes, baps_stream stream);
+size_t baps_kv_pages_workspace(int rows, int n_pages);
 
 /* Human-readable name of a status code (static string, never NULL). */
 const char *baps_status_string(baps_status status);

@@ -23,11 +23,15 @@ MODE_EXACT = 1
 MODE_EXP2_HIF8 = 2
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
+DTYPE_F16 = 2
+ALL_KEYS = 2 ** 31 - 1                       # a window that hides nothing
 
 EXPORTS = [
     "baps_hif8_encode", "baps_hif8_decode", "baps_exp2_hif8", "baps_softmax_rows", "baps_softmax_rows_codes",
     "baps_attention_fwd", "baps_attention_fwd_f32", "baps_attention_fwd_ex", "baps_attention_fwd_fp8",
     "baps_attention_restart_rates", "baps_attention_restart_rates_static",
+    "baps_attention_window_fwd", "baps_kv_append", "baps_kv_attention", "baps_kv_fork", "baps_kv_compact",
+    "baps_kv_attention_workspace", "baps_kv_pages_workspace",
     "baps_status_string", "baps_poll_async_error", "baps_launch_count",
 ]
 
@@ -75,8 +79,17 @@ def load() -> ctypes.CDLL:
     lib.baps_softmax_rows_codes.argtypes = [vp, vp, vp, vp, i64, i64, i, vp]
     lib.baps_attention_fwd_fp8.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i,
                                            ctypes.POINTER(_Opts), ctypes.POINTER(_Stats), vp]
-    for n in EXPORTS[:11]:
+    lib.baps_attention_window_fwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, ctypes.c_float, i, vp]
+    lib.baps_kv_append.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i, i, i, i, vp]
+    lib.baps_kv_attention.argtypes = [vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, i, ctypes.c_float, i, vp, sz, vp]
+    lib.baps_kv_fork.argtypes = [vp, vp, vp, i, vp, vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
+    lib.baps_kv_compact.argtypes = [vp, vp, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
+    for n in EXPORTS[:16]:
         getattr(lib, n).restype = i
+    lib.baps_kv_attention_workspace.argtypes = [i, i, i, i, i]
+    lib.baps_kv_attention_workspace.restype = sz
+    lib.baps_kv_pages_workspace.argtypes = [i, i]
+    lib.baps_kv_pages_workspace.restype = sz
     lib.baps_status_string.argtypes = [i]
     lib.baps_status_string.restype = ctypes.c_char_p
     lib.baps_poll_async_error.argtypes = [vp]
@@ -328,3 +341,204 @@ def baps_attention_restart_rates_static(q, k, v, *, causal: bool, out: torch.Ten
            load().baps_attention_restart_rates_static(_ptr(q), _ptr(k), _ptr(v), _ptr(out), B, H, Hkv, S, D,
                                                       int(bool(causal)), int(block_q), int(block_k), int(lam),
                                                       _ptr(rates), _stream()))
+
+
+# ---- serving: windowed prompts, the 8-bit cache, its attention and its pages -----------------------------------------
+
+_DTYPE16 = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+
+
+def _dtype16(t: torch.Tensor, name: str) -> int:
+    code = _DTYPE16.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected bfloat16 or float16")
+    return code
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+    """Strides (elements) of all dimensions but the last of a tensor whose rows are contiguous; a dimension of size one
+    may have any."""
+    if not (t.is_cuda and t.device == like.device and t.dtype == like.dtype and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return [s if n > 1 else 8 for s, n in zip(st[:-1], t.shape[:-1])]
+
+
+def _ints(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+    if not (t.dtype == torch.int32 and t.device == like.device and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _floats(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str):
+    if t is None:
+        return None
+    if not (t.dtype == torch.float32 and t.device == like.device and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _on(t: torch.Tensor):
+    """The library launches on the current device: refuse tensors of another."""
+    if not t.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _window(window: Optional[int]) -> int:
+    return ALL_KEYS if window is None else min(int(window), ALL_KEYS)
+
+
+def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0, scale: float = 0.0,
+                              lengths: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                              lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of prompts with a sliding window of ``window`` keys (None: all) and the first ``sinks`` keys always
+    visible; causal, plain softmax.  q [B,H,S,D], k, v [B,Hkv,S,D] bfloat16 or float16, any strides with contiguous rows
+    (for example a [B,S,heads,D] projection seen as [B,heads,S,D]).  ``lengths`` (int32 [B]): tokens of each
+    sequence of a padded batch; rows behind them are left as they are in ``out`` and ``lse`` (float32 [B,H,S])."""
+    code = _dtype16(q, "q")
+    _on(q)
+    B, H, Hkv, S, D = _attn_shapes(q, k, v)
+    if out is None:
+        out = torch.empty_like(q)
+    st = (ctypes.c_int64 * 12)(*_rows(q, q, q.shape, "q"), *_rows(k, q, k.shape, "k"), *_rows(v, q, k.shape, "v"),
+                               *_rows(out, q, q.shape, "out"))
+    _check("baps_attention_window_fwd",
+           load().baps_attention_window_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                            _floats(lse, q, (B, H, S), "lse"),
+                                            None if lengths is None else _ints(lengths, q, (B,), "lengths"), st, B, H, Hkv, S, D,
+                                            _window(window), int(sinks), float(scale), code, _stream()))
+    return out
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int)]
+
+
+class KvCache:
+    """A pool of pages of 8-bit keys and values: codes uint8 [n_pages,Hkv,page,D] (E4M3), scales float32 [n_pages,Hkv]."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "struct", "ref")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4:
+            raise ValueError("k: expected codes [n_pages, Hkv, page, D]")
+        for t, n in ((k, "k"), (v, "v")):
+            if not (t.is_cuda and t.device == k.device and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == k.shape):
+                raise ValueError(f"{n}: expected contiguous uint8 CUDA tensors of one shape")
+        for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _floats(t, k, k.shape[:2], n)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
+        self.ref = ctypes.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":
+        codes = [torch.zeros((n_pages, Hkv, page, D), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.ones((n_pages, Hkv), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *scales)
+
+
+def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_new: Optional[int] = None) -> None:
+    """Write new tokens into the cache: k_new, v_new [n,Hkv,D] bfloat16 or float16 (contiguous rows, any strides), tokens
+    starts[b] .. starts[b+1]-1 behind the lengths[b] that sequence b holds, in the pages of its row of ``table`` (int32
+    [B,width]).  ``max_new``: most tokens of one sequence (default: all of them).  ``lengths`` is not changed."""
+    code = _dtype16(k_new, "k_new")
+    _on(k_new)
+    n, (_, Hkv, _, D) = k_new.shape[0], cache.k.shape
+    B, width = table.shape
+    if k_new.device != cache.k.device:
+        raise ValueError("k_new is not on the cache's device")
+    st = (ctypes.c_int64 * 4)(*_rows(k_new, k_new, (n, Hkv, D), "k_new"), *_rows(v_new, k_new, (n, Hkv, D), "v_new"))
+    _check("baps_kv_append",
+           load().baps_kv_append(cache.ref, k_new.data_ptr(), v_new.data_ptr(), st, n, _ints(starts, k_new, (B + 1,), "starts"),
+                                 _ints(lengths, k_new, (B,), "lengths"), _ints(table, k_new, (B, width), "table"), width, B,
+                                 n if max_new is None else int(max_new), code, _stream()))
+
+
+def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int] = None, sinks: int = 0, scale: float = 0.0,
+                      out: Optional[torch.Tensor] = None, want_lse: bool = False, lse: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """Attention of the last T tokens of every sequence over the cache: q [B,H,T,D] bfloat16 or float16 (contiguous rows, any
+    strides), query t at position lengths[b]-T+t, T <= 16.  Returns out, or (out, lse float32 [B,H,T]) if ``want_lse``.
+    ``workspace``: a uint8 tensor of ``kv_attention_workspace`` bytes, allocated here if not given; calls that may run at
+    the same time need one each."""
+    code = _dtype16(q, "q")
+    _on(q)
+    if q.dim() != 4 or q.device != cache.k.device:
+        raise ValueError("q must be [B,H,T,D] on the cache's device")
+    B, H, T, D = q.shape
+    _, Hkv, _, Dc = cache.k.shape
+    if D != Dc or table.dim() != 2:
+        raise ValueError("q does not match the cache, or table is not [B,width]")
+    if out is None:
+        out = torch.empty_like(q)
+    if want_lse and lse is None:
+        lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
+    lib = load()
+    if workspace is None:
+        workspace = torch.empty(max(16, lib.baps_kv_attention_workspace(B, H, Hkv, T, D)), dtype=torch.uint8, device=q.device)
+    elif not (workspace.dtype == torch.uint8 and workspace.device == q.device and workspace.is_contiguous()):
+        raise ValueError("workspace: expected a contiguous uint8 tensor on q's device")
+    st = (ctypes.c_int64 * 6)(*_rows(q, q, q.shape, "q"), *_rows(out, q, q.shape, "out"))
+    _check("baps_kv_attention",
+           lib.baps_kv_attention(q.data_ptr(), out.data_ptr(), _floats(lse, q, (B, H, T), "lse"), cache.ref,
+                                 _ints(table, q, (B, table.shape[1]), "table"), table.shape[1], _ints(lengths, q, (B,), "lengths"), st,
+                                 B, H, T, _window(window), int(sinks), float(scale), code, workspace.data_ptr(),
+                                 workspace.numel(), _stream()))
+    return (out, lse) if want_lse else out
+
+
+def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int) -> int:
+    """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: sizes that it refuses)."""
+    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D))
+
+
+def _pages_workspace(lib, rows: int, cache: KvCache) -> torch.Tensor:
+    return torch.empty(lib.baps_kv_pages_workspace(rows, cache.k.shape[0]), dtype=torch.uint8, device=cache.k.device)
+
+
+def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int = 0, window: Optional[int] = None,
+                 sinks: int = 0):
+    """Rebuild the rows of a batch: new row i continues old row parents[i] (outside the table: an empty row), full
+    pages shared, last pages copied for all children of a parent but the first, pages outside the window let go, free pages
+    (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a row that found
+    no room has length -1."""
+    like = cache.k
+    _on(like)
+    rows, width = table.shape
+    n_pages, new_rows = like.shape[0], parents.numel()
+    lib = load()
+    new = torch.empty((new_rows, width), dtype=torch.int32, device=like.device)
+    new_lengths = torch.empty(new_rows, dtype=torch.int32, device=like.device)
+    new_refs = torch.empty(n_pages, dtype=torch.int32, device=like.device)
+    ws = _pages_workspace(lib, new_rows, cache)
+    _check("baps_kv_fork",
+           lib.baps_kv_fork(cache.ref, _ints(table, like, (rows, width), "table"), _ints(lengths, like, (rows,), "lengths"), rows,
+                            _ints(refs, like, (n_pages,), "refs"), _ints(parents, like, (new_rows,), "parents"), new_rows, width,
+                            int(reserve), _window(window), int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(),
+                            ws.data_ptr(), ws.numel(), _stream()))
+    return new, new_lengths, new_refs
+
+
+def baps_kv_compact(cache: KvCache, table, refs):
+    """Move the pages in use to the front of the pool.  Returns (new_table, new_refs, page_map, n_live), all int32."""
+    like = cache.k
+    _on(like)
+    rows, width = table.shape
+    n_pages = like.shape[0]
+    lib = load()
+    new = torch.empty((rows, width), dtype=torch.int32, device=like.device)
+    new_refs = torch.empty(n_pages, dtype=torch.int32, device=like.device)
+    page_map = torch.empty(n_pages, dtype=torch.int32, device=like.device)
+    n_live = torch.empty(1, dtype=torch.int32, device=like.device)
+    ws = _pages_workspace(lib, 0, cache)
+    _check("baps_kv_compact",
+           lib.baps_kv_compact(cache.ref, _ints(table, like, (rows, width), "table"), rows, width, _ints(refs, like, (n_pages,), "refs"),
+                               new.data_ptr(), new_refs.data_ptr(), page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(),
+                               ws.numel(), _stream()))
+    return new, new_refs, page_map, n_live

@@ -1,13 +1,16 @@
 """Build the CUDA library in-tree: ``python -m paper_2602_02071_b200.build``.
 
-Compiles ``csrc/baps_lib.cu`` (one translation unit that includes every kernel) for sm_100a into
+Compiles the translation units of ``csrc/`` (``baps_lib.cu``: conversions, row softmax, BAPS attention; ``baps_serving.cu``:
+windowed attention, the 8-bit key-value cache and its pages) for sm_100a, side by side, and links them into
 ``paper_2602_02071_b200/libbaps.so``.  nvcc cross-compiles, so no GPU is needed to build.
 """
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -20,32 +23,59 @@ WAIT_TEST_FLAGS = ["-DBAPS_WAIT_LIMIT_NS=1000000ull", "-DBAPS_TEST_SKIP_LOAD=1"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
+    "-Xcompiler", "-fPIC", "-Xptxas", "-v",
 ]
+UNITS = ["baps_lib.cu", "baps_serving.cu"]
 
 
-def _sources():
-    out = [os.path.join(_HERE, "..", "include", "baps.h")]
-    for name in sorted(os.listdir(CSRC)):
-        if name.endswith((".cu", ".cuh", ".h")):
-            out.append(os.path.join(CSRC, name))
-    return out
+def _sources(path: str, seen=None):
+    """``path`` and every file that it includes by a quoted name, however deep."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path not in seen:
+        seen.add(path)
+        with open(path) as f:
+            for name in re.findall(r'^\s*#include "([^"]+)"', f.read(), re.M):
+                _sources(os.path.join(os.path.dirname(path), name), seen)
+    return seen
+
+
+def _compile_unit(unit: str, lib: str, extra_flags, force: bool):
+    """One object file next to the library, if it is missing or older than a source; returns (path, compiler's output)."""
+    obj = f"{lib}.{os.path.splitext(unit)[0]}.o"
+    src = os.path.join(CSRC, unit)
+    log = obj + ".log"
+    if not force and os.path.exists(obj) and os.path.exists(log) and \
+            os.path.getmtime(obj) >= max(os.path.getmtime(p) for p in _sources(src)):
+        with open(log) as f:
+            return obj, f.read()
+    cmd = [os.environ.get("NVCC", "nvcc"), *NVCC_FLAGS, *extra_flags, "-c", "-o", obj + ".tmp", src]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    text = " ".join(cmd) + "\n" + res.stdout + res.stderr
+    if res.returncode != 0:
+        sys.stderr.write(text)
+        raise RuntimeError(f"nvcc failed on {unit}")
+    with open(log, "w") as f:
+        f.write(text)
+    os.replace(obj + ".tmp", obj)
+    return obj, text
 
 
 def _compile(lib: str, extra_flags, log_name: str, force: bool, verbose: bool) -> str:
-    newest = max(os.path.getmtime(p) for p in _sources())
+    newest = max(os.path.getmtime(p) for u in UNITS for p in _sources(os.path.join(CSRC, u)))
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= newest:
         return lib
-    nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc, *NVCC_FLAGS, *extra_flags, "-o", lib, os.path.join(CSRC, "baps_lib.cu")]
+    with ThreadPoolExecutor(len(UNITS)) as pool:
+        done = list(pool.map(lambda u: _compile_unit(u, lib, extra_flags, force), UNITS))
+    cmd = [os.environ.get("NVCC", "nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "--shared", "-o", lib, *(o for o, _ in done)]
     res = subprocess.run(cmd, capture_output=True, text=True)
-    log = res.stdout + res.stderr
+    log = "".join(t for _, t in done) + " ".join(cmd) + "\n" + res.stdout + res.stderr
     with open(os.path.join(_HERE, log_name), "w") as f:
-        f.write(" ".join(cmd) + "\n" + log)
+        f.write(log)
     if verbose or res.returncode != 0:
         sys.stderr.write(log)
     if res.returncode != 0:
-        raise RuntimeError(f"nvcc failed building {os.path.basename(lib)} (see {log_name})")
+        raise RuntimeError(f"nvcc failed linking {os.path.basename(lib)} (see {log_name})")
     return lib
 
 

@@ -83,103 +83,6 @@ struct TcLayout {
     static constexpr int kDynBytes = kTotal + 1024;                  // slack for 1024-byte alignment
 };
 
-__device__ __forceinline__ float lds_f32(uint32_t addr)
-{
-    float v;
-    asm("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
-}
-// Global load that stays behind the wait for the kernel ahead (await_previous_kernel), as volatile statements do.
-// (Not ld.global.nc, which asks for data that no kernel writes during this one's lifetime: that begins before the
-// kernel ahead has ended.  And not for the compiler to move: 32 / 8 heads x 8192 with 8-bit Q / K 675 -> 712 us.)
-__device__ __forceinline__ float ldg_f32(const float *p)
-{
-    float v;
-    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ float ex2_approx(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-// upper halves of two words as one: a's in the low half, b's in the high
-__device__ __forceinline__ uint32_t upper_halves(float a, float b)
-{
-    return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-}
-__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("min.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-// low half of a * byte 0 of b + high half of a * byte 1 of b + c
-__device__ __forceinline__ uint32_t dot_u16x2(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t d;
-    asm("dp2a.lo.u32.u32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-// Hardware (named) barriers among the softmax warps: id 0 is __syncthreads.
-__device__ __forceinline__ void named_bar_sync(uint32_t id, uint32_t nthreads)
-{
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
-}
-// Barrier that also ORs a predicate over all participating threads.
-__device__ __forceinline__ bool named_bar_or(uint32_t id, uint32_t nthreads, bool pred)
-{
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 q, %1, 0;\n\t"
-        "bar.red.or.pred p, %2, %3, q;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(r)
-        : "r"((uint32_t)pred), "r"(id), "r"(nthreads)
-        : "memory");
-    return r != 0;
-}
-__device__ __forceinline__ float4 lds_f32x4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float2 lds_f32x2(uint32_t addr)
-{
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ void sts_u32x4(uint32_t addr, uint4 v)
-{
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ uint4 lds_u32x4(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ void sts_f32(uint32_t addr, float v)
-{
-    asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
-}
-// 2^k for an integer-valued k (exact); 0 below the normal range, saturating far above it
-__device__ __forceinline__ float pow2_int(float k)
-{
-    const int e = 127 + (int)k;
-    return e > 0 ? __int_as_float(min(e, 254) << 23) : 0.f;
-}
-
 // ---- fast path -------------------------------------------------------------------------------
 // Weights of 16 columns when every T = S*c - mref of the row is <= 0 (a plain 8-bit tile whose
 // row maximum did not exceed the running max, or a restarted tile).

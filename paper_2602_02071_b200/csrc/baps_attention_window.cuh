@@ -1,0 +1,409 @@
+// Attention of whole prompts with a sliding window and a few first tokens that stay visible, on tcgen05 (bf16 or fp16).
+//
+// Row r of a sequence sees key c where c <= r and (c > r - window or c < sinks).  The plain softmax, one pass over the keys:
+//     m = running maximum, l = sum 2^(c s - m), O~ = sum 2^(c s - m) v;   O = O~ / l, lse = ln 2 (m + log2 l)
+// with s = q . k and c = log2(e) * scale.  m is held back: it moves only when a row's maximum passes it by more than 8
+// (weights stay below 2^8, exact in what follows), so that O~, which lives in tensor memory, is hardly ever rescaled.
+// S, l and O~ are float32; the weights are rounded to the inputs' type for the P V product (half a step, 2^-9 or 2^-12
+// of each weight) and summed before that rounding.
+//
+// One CTA owns two consecutive 128-row query tiles (t = 0, 1) of one head, which share the K / V stream: the tiles that
+// hold first tokens, then those from the window's left edge to the diagonal.  A stream takes part in the key tiles that
+// some row of its own sees.
+//   warps 0-3, 4-7  softmax of stream 0, 1: a thread per row
+//   warp 8          TMA producer: Q tiles, then K_0, V_0, K_1, ... through a ring of 128 x D tiles
+//   warp 9          MMA issuer, per key tile and stream: P V, then Q K^T of the stream's next key tile into the same columns
+//   warps 10, 11    zero what stands behind a sequence's end in its last V tile (a weight of 0 does not hide a NaN)
+// TMEM (512 columns): S_0 | S_1 | O_0 | O_1, 128 columns each; the 16-bit weights of column
+// quarter q overwrite columns [32 q, 32 q + 16) of S_t.
+// Tensor memory is taken after the kernel ahead has ended and before the next one may start.  All waits are bounded; after an
+// expired one every later wait returns at once and the roles run on to the common teardown without storing.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include "baps_common.cuh"
+#include "baps_sm100.cuh"
+#include "baps_tma_host.cuh"
+
+namespace baps {
+
+struct WindowParams {
+    void *out;
+    float *lse;
+    const int32_t *lengths;
+    int64_t os_b, os_h, os_s;      // strides of out, elements
+    int B, H, Hkv, S, window, sinks, npairs;
+    float c;
+};
+
+constexpr int kWinThreads = 384;
+
+template <int D>
+struct WinLayout {
+    static constexpr int kTileBytes = 128 * D * 2, kStages = D == 128 ? 4 : 8;
+    static constexpr int kQOff = 0;
+    static constexpr int kKvOff = 2 * kTileBytes;
+    static constexpr int kBarOff = kKvOff + kStages * kTileBytes;
+    // q_full, s_full[2], p_full[2], o_done[2], v_there, v_clean, kv_full[stages], kv_empty[stages]
+    static constexpr int kMiscOff = (kBarOff + (9 + 2 * kStages) * 8 + 15) & ~15;
+    static constexpr int kDynBytes = kMiscOff + 16 + 1024;
+};
+
+// Key tiles that rows [r0, r1] see (r0 <= r1): first tokens' tiles 0 .. ns - 1, then w0 .. w1.
+struct KeyTiles {
+    int ns, w0, w1;
+    __host__ __device__ int count() const { return ns + w1 - w0 + 1; }
+    __host__ __device__ int tile(int i) const { return i < ns ? i : w0 + i - ns; }
+    __host__ __device__ bool has(int tile) const { return tile < ns || (tile >= w0 && tile <= w1); }
+};
+__host__ __device__ inline KeyTiles key_tiles(int r0, int r1, int window, int sinks, int log2_tile)
+{
+    const int lo = r0 - window >= 0 ? r0 - window + 1 : 0;          // (no overflow: r0 >= 0, window >= 1)
+    KeyTiles k;
+    k.w0 = lo >> log2_tile;
+    k.w1 = r1 >> log2_tile;
+    const int seen = sinks < lo ? sinks : lo;                       // first tokens left of the window
+    k.ns = seen > 0 ? ((seen - 1) >> log2_tile) + 1 : 0;
+    if (k.ns > k.w0) k.ns = k.w0;
+    return k;
+}
+
+template <typename T16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi)
+{
+    if constexpr (sizeof(T16) == 2 && __is_same(T16, __half)) {
+        uint32_t d;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+        return d;
+    } else {
+        return pack_bf16x2(lo, hi);
+    }
+}
+
+__device__ __forceinline__ float max8w(const uint32_t *x)
+{
+    return max3(max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2])),
+                max3(__uint_as_float(x[3]), __uint_as_float(x[4]), __uint_as_float(x[5])),
+                fmaxf(__uint_as_float(x[6]), __uint_as_float(x[7])));
+}
+
+template <typename T16, int D>
+__global__ void __launch_bounds__(kWinThreads, 1)
+window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                        const __grid_constant__ CUtensorMap mv, const WindowParams p)
+{
+    using namespace sm100;
+    using L = WinLayout<D>;
+    constexpr bool kHalf = __is_same(T16, __half);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem);
+    auto bar = [&](int i) { return sbase + L::kBarOff + 8u * (uint32_t)i; };
+    constexpr int BQ = 0, BS = 1, BP = 3, BD = 5, BV = 7, BC = 8, BKF = 9, BKE = 9 + L::kStages;
+    uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + L::kMiscOff);
+    volatile int *s_abort = reinterpret_cast<volatile int *>(smem + L::kMiscOff + 4);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // blocks: query heads of a kv head next to each other, later rows (more keys, while the window fills) first
+    const int heads = p.B * p.H;
+    const int h = (int)(blockIdx.x % (unsigned)heads) % p.H, b = (int)(blockIdx.x % (unsigned)heads) / p.H;
+    const int q0 = 2 * (p.npairs - 1 - (int)(blockIdx.x / (unsigned)heads));
+    const int hk = h / (p.H / p.Hkv);
+
+    await_previous_kernel();
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.S) : p.S;
+    if (q0 * 128 >= len) return;
+    // last rows of the two query tiles; the second is absent where the sequence ends in the first
+    const bool two = (q0 + 1) * 128 < len;
+    const int last0 = min(q0 * 128 + 127, len - 1), last1 = min(q0 * 128 + 255, len - 1);
+    const KeyTiles kt = key_tiles(q0 * 128, last1, p.window, p.sinks, 7);
+    const KeyTiles mine0 = key_tiles(q0 * 128, last0, p.window, p.sinks, 7);
+    const KeyTiles mine1 = key_tiles(min(q0 * 128 + 128, last1), last1, p.window, p.sinks, 7);
+    const int J = kt.count();
+    auto takes = [&](int t, int j) { return t == 0 ? mine0.has(kt.tile(j)) : two && mine1.has(kt.tile(j)); };
+    auto stage_of = [&](int l) { return l % L::kStages; };
+    auto parity_of = [&](int l) { return (uint32_t)((l / L::kStages) & 1); };
+    // the sequence's last V tile holds rows behind its end (rows behind S come as zeros)
+    const bool ragged = len < p.S && (len & 127) != 0 && kt.w1 == (len - 1) >> 7;
+
+    if (tid == 0) {
+        mbar_init(bar(BQ), 1);
+        for (int t = 0; t < 2; ++t) { mbar_init(bar(BS + t), 1); mbar_init(bar(BP + t), 4); mbar_init(bar(BD + t), 1); }
+        mbar_init(bar(BV), 1);
+        mbar_init(bar(BC), 2);
+        for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(BKF + s), 1); mbar_init(bar(BKE + s), 1); }
+        mbar_fence_init();
+        *s_abort = 0;
+    }
+    if (warp == 9) { tmem_alloc(smem_u32(s_tmem), 512); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    allow_next_kernel();
+    const uint32_t tmem = *s_tmem;
+
+    if (warp == 8) {
+        // ======================= TMA producer ======================================================
+        if (lane == 0) {
+            mbar_arrive_expect_tx(bar(BQ), (two ? 2u : 1u) * L::kTileBytes);
+            for (int t = 0; t < (two ? 2 : 1); ++t)
+                for (int hh = 0; hh < D / 64; ++hh)
+                    tma_load_4d(sbase + L::kQOff + t * L::kTileBytes + hh * 16384, &mq, hh * 64, (q0 + t) * 128, h, b, bar(BQ));
+            int issued = 0;
+            for (int l = 0; l < 2 * J; ++l) {
+                const int s = stage_of(l);
+                if (!mbar_wait(bar(BKE + s), parity_of(l) ^ 1u, s_abort, &g_async_status, 0x400 + s)) break;
+                mbar_arrive_expect_tx(bar(BKF + s), L::kTileBytes);
+                for (int hh = 0; hh < D / 64; ++hh)
+                    tma_load_4d(sbase + L::kKvOff + s * L::kTileBytes + hh * 16384, (l & 1) ? &mv : &mk, hh * 64,
+                                kt.tile(l >> 1) * 128, hk, b, bar(BKF + s));
+                issued = l + 1;
+            }
+            if (*s_abort) {
+                // copies in flight land before the CTA's shared memory is released
+                for (int l = issued > L::kStages ? issued - L::kStages : 0; l < issued; ++l) {
+                    const uint64_t t0 = globaltimer_ns();
+                    while (!mbar_try_wait(bar(BKF + stage_of(l)), parity_of(l)) && globaltimer_ns() - t0 < 2000000ull) {}
+                }
+            }
+        }
+    } else if (warp == 9) {
+        // ======================= MMA issuer ========================================================
+        constexpr uint32_t fmt = kHalf ? 0u : (1u << 7) | (1u << 10);
+        constexpr uint32_t idesc_qk = (make_idesc_bf16(128, 128, false) & ~((7u << 7) | (7u << 10))) | fmt;
+        constexpr uint32_t idesc_pv = (make_idesc_bf16(128, D, true) & ~((7u << 7) | (7u << 10))) | fmt;
+        auto wait_all = [&](uint32_t bar_addr, uint32_t parity, int code) -> bool {
+            return __all_sync(0xffffffffu, mbar_wait(bar_addr, parity, s_abort, &g_async_status, code));
+        };
+        const bool leader = elect_one();
+        auto mma_qk = [&](int t, int j) {
+            const uint32_t qd = sdesc_lo(sbase + L::kQOff + t * L::kTileBytes, 16);
+            const uint32_t kd = sdesc_lo(sbase + L::kKvOff + stage_of(2 * j) * L::kTileBytes, 16);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const uint32_t off = (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4);
+                mma_ss_lo(tmem + t * 128, qd + off, kd + off, idesc_qk, ks > 0);
+            }
+            mma_commit(bar(BS + t));
+        };
+        auto mma_pv = [&](int t, int j, bool more) {
+            const uint32_t vd = sdesc_lo(sbase + L::kKvOff + stage_of(2 * j + 1) * L::kTileBytes, 16384);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+                mma_ts_lo(tmem + 256 + t * 128, tmem + t * 128 + (ks >> 1) * 32 + (ks & 1) * 8, vd + ks * 128, idesc_pv, more || ks > 0);
+        };
+        // A stream's next Q K^T is issued behind its P V, into the same columns.
+        int done[2] = {0, 0};                          // key tiles that the stream has been through
+        auto next_of = [&](int t, int j) { while (j < J && !takes(t, j)) ++j; return j; };
+        int nj[2] = {next_of(0, 0), next_of(1, 0)};    // the tile whose scores were asked for last (J: no more)
+        int k_there = 0, k_freed = 0;                  // K tiles waited for, and given back
+        bool ok = wait_all(bar(BQ), 0, 0x410);
+        auto need_k = [&](int j) {
+            for (; ok && k_there <= j; ++k_there) ok = wait_all(bar(BKF + stage_of(2 * k_there)), parity_of(2 * k_there), 0x411);
+        };
+        // K_f is free when both streams have asked for their scores of it, or of a later tile
+        auto free_k = [&] {
+            for (; k_freed < J && k_freed <= min(nj[0], nj[1]); ++k_freed) mma_commit(bar(BKE + stage_of(2 * k_freed)));
+        };
+        for (int t = 0; t < 2; ++t)
+            if (nj[t] < J) {
+                need_k(nj[t]);
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (leader) mma_qk(t, nj[t]);
+                __syncwarp();
+            }
+        if (ok && leader) free_k();
+        k_freed = min(J, min(nj[0], nj[1]) + 1);
+        for (int j = 0; ok && j < J; ++j) {
+            ok = wait_all(bar(BKF + stage_of(2 * j + 1)), parity_of(2 * j + 1), 0x420);
+            if (ok && ragged && j == J - 1) {
+                if (leader) mbar_arrive(bar(BV));
+                __syncwarp();
+                ok = wait_all(bar(BC), 0, 0x421);
+            }
+            for (int t = 0; ok && t < 2; ++t) {
+                if (nj[t] != j) continue;
+                const int nx = next_of(t, j + 1);
+                if (nx < J) need_k(nx);
+                ok = ok && wait_all(bar(BP + t), (uint32_t)(done[t] & 1), 0x430 + t);
+                if (!ok) break;
+                tc_fence_after_sync();
+                nj[t] = nx;
+                if (leader) {
+                    mma_pv(t, j, done[t] > 0);
+                    if (nx < J) mma_qk(t, nx);
+                    else mma_commit(bar(BD + t));
+                    free_k();
+                }
+                k_freed = min(J, min(nj[0], nj[1]) + 1);
+                ++done[t];
+                __syncwarp();
+            }
+            if (ok && leader) mma_commit(bar(BKE + stage_of(2 * j + 1)));
+            __syncwarp();
+        }
+    } else if (warp >= 10) {
+        // ======================= rows behind the sequence's end ====================================
+        if (ragged) {
+            const int l = 2 * J - 1, first = len & 127;
+            if (__all_sync(0xffffffffu, mbar_wait(bar(BV), 0, s_abort, &g_async_status, 0x440))) {
+                const uint32_t stage = sbase + L::kKvOff + stage_of(l) * L::kTileBytes;
+                for (int i = (warp - 10) * 32 + lane; i < (128 - first) * (D / 8); i += 64) {
+                    const int row = first + i / (D / 8), part = i % (D / 8);
+                    sts_u32x4(stage + (uint32_t)((part >> 3) * 16384 + row * 128 + (part & 7) * 16), make_uint4(0, 0, 0, 0));
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BC));
+            }
+        }
+    } else if (warp < (two ? 8 : 4)) {
+        // ======================= softmax warps =====================================================
+        const int t = warp >> 2, q4 = warp & 3;
+        const int row = q4 * 32 + lane;                               // of the query tile
+        const int r = (q0 + t) * 128 + row;                           // of the sequence
+        const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
+        const uint32_t s_addr = tmem + lane_sel + t * 128, o_addr = tmem + lane_sel + 256 + t * 128;
+        const int r_first = (q0 + t) * 128, r_last = r_first + 127;
+        const float c = p.c;
+        const uint64_t c2 = pack2(c, c);
+        float m = -INFINITY, l = 0.f;
+        int n = 0;
+        for (int j = 0; j < J; ++j) {
+            if (!takes(t, j)) continue;
+            const int c0 = kt.tile(j) * 128;
+            // every row of the stream sees every key of the tile
+            const bool all = c0 + 127 <= r_first && (c0 > r_last - p.window || c0 + 127 < p.sinks);
+            mbar_wait(bar(BS + t), (uint32_t)(n & 1), s_abort, &g_async_status, 0x450 + t);
+            tc_fence_after_sync();
+            // columns c0 + 32 i .. + 31 that the row sees, as bits
+            auto visible = [&](int i) -> uint32_t {
+                const int b0 = c0 + 32 * i;
+                auto below = [&](int x) -> uint32_t { x -= b0; return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; };
+                const uint32_t near = below(r + 1) & ~below(r - p.window + 1);
+                return near | (below(p.sinks) & below(r + 1));
+            };
+            auto load = [&](int i, uint32_t (&x)[32]) { tmem_ld32(s_addr + 32 * i, x); };
+            auto mask = [&](int i, uint32_t (&x)[32]) {
+                if (!all) {
+                    const uint32_t see = visible(i);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) x[k] = (see >> k & 1u) ? x[k] : 0xFF800000u;
+                }
+            };
+            auto max32 = [&](const uint32_t (&x)[32]) {
+                return max3(max3(max8w(&x[0]), max8w(&x[8]), max8w(&x[16])), max8w(&x[24]), -INFINITY);
+            };
+            uint32_t x[32], y[32];
+            load(0, x); load(1, y);
+            tmem_wait_ld();
+            mask(0, x); mask(1, y);
+            float mx = fmaxf(max32(x), max32(y));
+            load(2, x); load(3, y);
+            tmem_wait_ld();
+            mask(2, x); mask(3, y);
+            mx = max3(mx, max32(x), max32(y)) * c;
+            if (__any_sync(0xffffffffu, mx > m + 8.f)) {
+                const float m_new = fmaxf(m, mx);
+                const float f = m == -INFINITY ? 1.f : ex2_approx(m - m_new);      // (nothing there yet: l = 0, O~ = 0)
+                if (n > 0) {
+#pragma unroll 1
+                    for (int i0 = 0; i0 < D; i0 += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(o_addr + i0, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(o_addr + i0, o);
+                    }
+                }
+                l *= f;
+                m = m_new;
+            }
+            const float mu = m == -INFINITY ? 0.f : -m;
+            const uint64_t m2 = pack2(mu, mu);
+            uint64_t s01 = 0ull, s23 = 0ull;
+            auto weights = [&](int i, const uint32_t (&x)[32]) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    float w[4];
+                    unpack2(fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), w[0], w[1]);
+                    unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), c2, m2), w[2], w[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = ex2_approx(w[e]);
+                    s01 = add2(s01, pack2(w[0], w[1]));
+                    s23 = add2(s23, pack2(w[2], w[3]));
+                    pk[k >> 1] = pack16<T16>(w[0], w[1]);
+                    pk[(k >> 1) + 1] = pack16<T16>(w[2], w[3]);
+                }
+                tmem_st16(s_addr + 32 * i, pk);
+            };
+            weights(2, x);
+            weights(3, y);
+            load(0, x); load(1, y);
+            tmem_wait_ld();
+            mask(0, x); mask(1, y);
+            weights(0, x);
+            weights(1, y);
+            tmem_wait_st();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(BP + t));
+            float a0, a1, a2, a3;
+            unpack2(s01, a0, a1); unpack2(s23, a2, a3);
+            l += (a0 + a1) + (a2 + a3);
+            ++n;
+        }
+        // ---- O = O~ / l, through the (now idle) Q tile so that the stores are whole rows --------------------
+        const bool good = mbar_wait(bar(BD + t), 0, s_abort, &g_async_status, 0x460 + t) && *s_abort == 0;
+        tc_fence_after_sync();
+        const float inv = 1.f / l;
+        constexpr int kChunks = D / 8;                               // 16-byte parts of a row
+        const uint32_t stage = sbase + L::kQOff + t * L::kTileBytes;
+#pragma unroll 1
+        for (int i0 = 0; i0 < D; i0 += 16) {
+            uint32_t rr[16];
+            tmem_ld16(o_addr + i0, rr);
+            tmem_wait_ld();
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack16<T16>(__uint_as_float(rr[2 * i]) * inv, __uint_as_float(rr[2 * i + 1]) * inv);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                sts_u32x4(stage + (uint32_t)(row * 2 * D + (((i0 >> 3) + i) ^ (row & (kChunks - 1))) * 16),
+                          make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        }
+        __syncwarp();
+        T16 *out = reinterpret_cast<T16 *>(p.out) + b * p.os_b + h * p.os_h;
+        constexpr int kRowsAtOnce = 32 / kChunks;
+#pragma unroll 4
+        for (int i = 0; i < kChunks; ++i) {
+            const int rw = q4 * 32 + i * kRowsAtOnce + lane / kChunks, part = lane % kChunks;
+            const uint4 v = lds_u32x4(stage + (uint32_t)(rw * 2 * D + (part ^ (rw & (kChunks - 1))) * 16));
+            const int64_t gr = (int64_t)(q0 + t) * 128 + rw;
+            if (good && gr < len) *reinterpret_cast<uint4 *>(out + gr * p.os_s + part * 8) = v;
+        }
+        if (good && p.lse && r < len) p.lse[((int64_t)b * p.H + h) * p.S + r] = (m + log2f(l)) * 0.69314718055994531f;
+    }
+
+    // ---- teardown -------------------------------------------------------------------------------
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 9) { __syncwarp(); tmem_dealloc(tmem, 512); }
+}
+
+template <typename T16, int D>
+static inline baps_status window_launch(const CUtensorMap *maps, const WindowParams &p, cudaStream_t stream)
+{
+    const long long blocks = (long long)p.B * p.H * p.npairs;
+    if (blocks > 0x7fffffffLL) return BAPS_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(window_attention_kernel<T16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             WinLayout<D>::kDynBytes) != cudaSuccess)
+        return BAPS_ERR_CUDA;
+    return launch_kernel(window_attention_kernel<T16, D>, (unsigned)blocks, kWinThreads, (size_t)WinLayout<D>::kDynBytes, stream,
+                         maps[0], maps[1], maps[2], p);
+}
+
+} // namespace baps

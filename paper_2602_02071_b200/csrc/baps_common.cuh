@@ -10,15 +10,26 @@
 namespace baps {
 
 // Device-side status word: 0 = fine; non-zero = a bounded wait expired (the value encodes
-// which role gave up).  Read and cleared by baps_poll_async_error().
-__device__ int g_async_status = 0;
+// which role gave up).  Read and cleared by baps_poll_async_error().  Each translation unit has its own.
+static __device__ int g_async_status = 0;
+
+// Reads and clears the word of the translation unit it is called in (the caller has waited for the stream).
+static inline baps_status take_async_status()
+{
+    int host = 0;
+    if (cudaMemcpyFromSymbol(&host, g_async_status, sizeof(int)) != cudaSuccess) return BAPS_ERR_CUDA;
+    if (host == 0) return BAPS_OK;
+    const int zero = 0;
+    return cudaMemcpyToSymbol(g_async_status, &zero, sizeof(int)) == cudaSuccess ? BAPS_ERR_TIMEOUT : BAPS_ERR_CUDA;
+}
+baps_status take_serving_status();       // that of baps_serving.cu
 
 // Host-side count of kernel launches issued by this library.
-static std::atomic<int64_t> g_launches{0};
+inline std::atomic<int64_t> g_launches{0};
 
 // Serialises the one-time, per-device set-up steps (table builds, symbol look-ups) when several
 // host threads make their first call at the same time.
-static std::mutex g_setup_mutex;
+inline std::mutex g_setup_mutex;
 
 constexpr float kLog2e = 1.4426950408889634074f;
 
@@ -68,6 +79,21 @@ inline bool have_device()
 {
     int dev = -1;
     return cudaGetDevice(&dev) == cudaSuccess && dev >= 0;
+}
+
+// Streaming multiprocessors of the current device.
+inline int num_sms()
+{
+    static int cached[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    if (cached[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+            n = 148;
+        cached[dev] = n;
+    }
+    return cached[dev];
 }
 
 inline cudaStream_t as_stream(baps_stream s) { return reinterpret_cast<cudaStream_t>(s); }

@@ -1,5 +1,6 @@
 // C-ABI entry points of the BAPS CUDA library (declared in include/baps.h).
-// One translation unit: the kernels live in the .cuh files included below.
+// The kernels live in the .cuh files included below; the entry points around the key-value cache and the windowed
+// attention are in baps_serving.cu.
 #include "baps_common.cuh"
 #include "baps_hif8.cuh"
 #include "baps_elementwise.cuh"
@@ -13,20 +14,6 @@
 using namespace baps;
 
 namespace {
-
-int num_sms()
-{
-    static int cached[64] = {0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-            n = 148;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
 
 template <int BLK>
 baps_status attention_f32_launch(const AttnF32Params &p, cudaStream_t st)
@@ -179,14 +166,8 @@ baps_status baps_poll_async_error(baps_stream stream)
     if (!have_device()) return BAPS_ERR_CUDA;
     cudaStream_t st = as_stream(stream);
     if (cudaStreamSynchronize(st) != cudaSuccess) return BAPS_ERR_CUDA;
-    int host = 0;
-    if (cudaMemcpyFromSymbol(&host, g_async_status, sizeof(int)) != cudaSuccess) return BAPS_ERR_CUDA;
-    if (host != 0) {
-        const int zero = 0;
-        if (cudaMemcpyToSymbol(g_async_status, &zero, sizeof(int)) != cudaSuccess) return BAPS_ERR_CUDA;
-        return BAPS_ERR_TIMEOUT;
-    }
-    return BAPS_OK;
+    const baps_status own = take_async_status(), serving = take_serving_status();
+    return own != BAPS_OK ? own : serving;
 }
 
 // First call on a device: build the 8192-entry code table and the 256-entry exponent map and wait for
