@@ -8,7 +8,9 @@ is missing the import of the library fails loudly -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -344,52 +346,57 @@ def baps_attention_restart_rates_static(q, k, v, *, causal: bool, out: torch.Ten
 
 
 # ---- serving: windowed prompts, the 8-bit cache, its attention and its pages -----------------------------------------
+#
+# The smallest of these calls take a few microseconds on the device, so the checks are written to be cheap: one condition
+# per tensor, structures and strides handed over as packed bytes (a ctypes structure takes 1 us to fill), outputs
+# allocated from a tensor of their kind (new_empty, 1.7 us; torch.empty with a type and a device, 2.3).
 
 _DTYPE16 = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+_device = torch._C._cuda_getDevice
 
 
 def _dtype16(t: torch.Tensor, name: str) -> int:
+    """Code of the type of a 16-bit CUDA tensor on the current device (the library launches on that one)."""
     code = _DTYPE16.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name}: expected bfloat16 or float16")
+    if code is None or not t.is_cuda:
+        raise ValueError(f"{name}: expected a bfloat16 or float16 CUDA tensor")
+    if t.get_device() != _device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_device()}")
     return code
 
 
-def _rows(t: torch.Tensor, like: torch.Tensor, shape, name: str):
-    """Strides (elements) of all dimensions but the last of a tensor whose rows are contiguous; a dimension of size one
-    may have any."""
-    if not (t.is_cuda and t.device == like.device and t.dtype == like.dtype and tuple(t.shape) == tuple(shape)):
-        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+def _stride3(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+    """Strides (elements) of the leading three dimensions of a tensor of contiguous rows; where a dimension has one
+    element only, its stride does not matter and may be anything."""
     st = t.stride()
-    if st[-1] != 1:
-        raise ValueError(f"{name}: the elements of a row must be contiguous")
-    return [s if n > 1 else 8 for s, n in zip(st[:-1], t.shape[:-1])]
+    if t.dtype != like.dtype or t.shape != shape or t.device != like.device or st[3] != 1:
+        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
+    a, b, c, _ = shape
+    return (st[0] if a > 1 else 8, st[1] if b > 1 else 8, st[2] if c > 1 else 8)
 
 
-def _ints(t: torch.Tensor, like: torch.Tensor, shape, name: str):
-    if not (t.dtype == torch.int32 and t.device == like.device and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
-        raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on {like.device}")
+def _stride2(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+    st = t.stride()
+    if t.dtype != like.dtype or t.shape != shape or t.device != like.device or st[2] != 1:
+        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
+    return (st[0] if shape[0] > 1 else 8, st[1] if shape[1] > 1 else 8)
+
+
+def _buffer(t: torch.Tensor, dtype, device, shape, name: str) -> int:
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return t.data_ptr()
-
-
-def _floats(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str):
-    if t is None:
-        return None
-    if not (t.dtype == torch.float32 and t.device == like.device and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
-        raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {tuple(shape)} on {like.device}")
-    return t.data_ptr()
-
-
-def _on(t: torch.Tensor):
-    """The library launches on the current device: refuse tensors of another."""
-    if not t.is_cuda:
-        raise ValueError("expected CUDA tensors")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _window(window: Optional[int]) -> int:
     return ALL_KEYS if window is None else min(int(window), ALL_KEYS)
+
+
+def _pack(fmt: str, *values) -> bytes:
+    try:
+        return struct.pack(fmt, *values)
+    except struct.error as e:
+        raise ValueError(f"a size is out of range: {e}") from None
 
 
 def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0, scale: float = 0.0,
@@ -400,41 +407,38 @@ def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0,
     (for example a [B,S,heads,D] projection seen as [B,heads,S,D]).  ``lengths`` (int32 [B]): tokens of each
     sequence of a padded batch; rows behind them are left as they are in ``out`` and ``lse`` (float32 [B,H,S])."""
     code = _dtype16(q, "q")
-    _on(q)
     B, H, Hkv, S, D = _attn_shapes(q, k, v)
     if out is None:
         out = torch.empty_like(q)
-    st = (ctypes.c_int64 * 12)(*_rows(q, q, q.shape, "q"), *_rows(k, q, k.shape, "k"), *_rows(v, q, k.shape, "v"),
-                               *_rows(out, q, q.shape, "out"))
-    _check("baps_attention_window_fwd",
-           load().baps_attention_window_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                            _floats(lse, q, (B, H, S), "lse"),
-                                            None if lengths is None else _ints(lengths, q, (B,), "lengths"), st, B, H, Hkv, S, D,
-                                            _window(window), int(sinks), float(scale), code, _stream()))
+    qs, ks = q.shape, k.shape
+    st = _pack("12q", *_stride3(q, q, qs, "q"), *_stride3(k, q, ks, "k"), *_stride3(v, q, ks, "v"), *_stride3(out, q, qs, "out"))
+    status = load().baps_attention_window_fwd(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+        None if lse is None else _buffer(lse, torch.float32, q.device, (B, H, S), "lse"),
+        None if lengths is None else _buffer(lengths, torch.int32, q.device, (B,), "lengths"), st, B, H, Hkv, S, D,
+        _window(window), int(sinks), float(scale), code, _stream())
+    if status:
+        _check("baps_attention_window_fwd", status)
     return out
-
-
-class _Cache(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
-                ("n_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int)]
 
 
 class KvCache:
     """A pool of pages of 8-bit keys and values: codes uint8 [n_pages,Hkv,page,D] (E4M3), scales float32 [n_pages,Hkv]."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "struct", "ref")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        if k.dim() != 4:
-            raise ValueError("k: expected codes [n_pages, Hkv, page, D]")
-        for t, n in ((k, "k"), (v, "v")):
-            if not (t.is_cuda and t.device == k.device and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == k.shape):
-                raise ValueError(f"{n}: expected contiguous uint8 CUDA tensors of one shape")
-        for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _floats(t, k, k.shape[:2], n)
+        shape, device = k.shape, k.device
+        if len(shape) != 4 or not k.is_cuda:
+            raise ValueError("k: expected CUDA codes [n_pages, Hkv, page, D]")
+        if k.dtype != torch.uint8 or v.dtype != torch.uint8 or v.shape != shape or v.device != device or \
+                not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k, v: expected contiguous uint8 CUDA tensors of one shape")
+        pages = shape[:2]
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.struct = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
-        self.ref = ctypes.addressof(self.struct)
+        # baps_kv_cache
+        self.struct = _pack("4Q4i", k.data_ptr(), v.data_ptr(), _buffer(k_scale, torch.float32, device, pages, "k_scale"),
+                            _buffer(v_scale, torch.float32, device, pages, "v_scale"), *shape)
 
     @classmethod
     def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":
@@ -442,22 +446,38 @@ class KvCache:
         scales = [torch.ones((n_pages, Hkv), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(*codes, *scales)
 
+    def here(self) -> torch.device:
+        """The cache's device, which has to be the current one."""
+        if self.k.get_device() != _device():
+            raise ValueError(f"the cache is on {self.k.device}, the current device is cuda:{_device()}")
+        return self.k.device
+
 
 def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_new: Optional[int] = None) -> None:
     """Write new tokens into the cache: k_new, v_new [n,Hkv,D] bfloat16 or float16 (contiguous rows, any strides), tokens
     starts[b] .. starts[b+1]-1 behind the lengths[b] that sequence b holds, in the pages of its row of ``table`` (int32
     [B,width]).  ``max_new``: most tokens of one sequence (default: all of them).  ``lengths`` is not changed."""
     code = _dtype16(k_new, "k_new")
-    _on(k_new)
+    device = cache.here()
     n, (_, Hkv, _, D) = k_new.shape[0], cache.k.shape
     B, width = table.shape
-    if k_new.device != cache.k.device:
-        raise ValueError("k_new is not on the cache's device")
-    st = (ctypes.c_int64 * 4)(*_rows(k_new, k_new, (n, Hkv, D), "k_new"), *_rows(v_new, k_new, (n, Hkv, D), "v_new"))
-    _check("baps_kv_append",
-           load().baps_kv_append(cache.ref, k_new.data_ptr(), v_new.data_ptr(), st, n, _ints(starts, k_new, (B + 1,), "starts"),
-                                 _ints(lengths, k_new, (B,), "lengths"), _ints(table, k_new, (B, width), "table"), width, B,
-                                 n if max_new is None else int(max_new), code, _stream()))
+    st = _pack("4q", *_stride2(k_new, k_new, (n, Hkv, D), "k_new"), *_stride2(v_new, k_new, (n, Hkv, D), "v_new"))
+    status = load().baps_kv_append(
+        cache.struct, k_new.data_ptr(), v_new.data_ptr(), st, n, _buffer(starts, torch.int32, device, (B + 1,), "starts"),
+        _buffer(lengths, torch.int32, device, (B,), "lengths"), _buffer(table, torch.int32, device, (B, width), "table"), width, B,
+        n if max_new is None else min(int(max_new), n), code, _stream())
+    if status:
+        _check("baps_kv_append", status)
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_workspace(device: int, B: int, H: int, Hkv: int, T: int, D: int) -> int:
+    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D))
+
+
+def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int) -> int:
+    """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: sizes that it refuses)."""
+    return _attention_workspace(_device(), B, H, Hkv, T, D)
 
 
 def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int] = None, sinks: int = 0, scale: float = 0.0,
@@ -468,77 +488,76 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     ``workspace``: a uint8 tensor of ``kv_attention_workspace`` bytes, allocated here if not given; calls that may run at
     the same time need one each."""
     code = _dtype16(q, "q")
-    _on(q)
-    if q.dim() != 4 or q.device != cache.k.device:
-        raise ValueError("q must be [B,H,T,D] on the cache's device")
-    B, H, T, D = q.shape
+    device = cache.here()
+    shape = q.shape
+    B, H, T, D = shape
     _, Hkv, _, Dc = cache.k.shape
-    if D != Dc or table.dim() != 2:
+    rows, width = table.shape
+    if D != Dc or rows != B:
         raise ValueError("q does not match the cache, or table is not [B,width]")
     if out is None:
         out = torch.empty_like(q)
-    if want_lse and lse is None:
-        lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
-    lib = load()
+    if lse is not None:
+        lse_ptr = _buffer(lse, torch.float32, device, (B, H, T), "lse")
+    elif want_lse:
+        lse = cache.k_scale.new_empty((B, H, T))
+        lse_ptr = lse.data_ptr()
+    else:
+        lse_ptr = None
     if workspace is None:
-        workspace = torch.empty(max(16, lib.baps_kv_attention_workspace(B, H, Hkv, T, D)), dtype=torch.uint8, device=q.device)
-    elif not (workspace.dtype == torch.uint8 and workspace.device == q.device and workspace.is_contiguous()):
+        n = _attention_workspace(_device(), B, H, Hkv, T, D) or 16
+        workspace = cache.k.new_empty((n,))
+    elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor on q's device")
-    st = (ctypes.c_int64 * 6)(*_rows(q, q, q.shape, "q"), *_rows(out, q, q.shape, "out"))
-    _check("baps_kv_attention",
-           lib.baps_kv_attention(q.data_ptr(), out.data_ptr(), _floats(lse, q, (B, H, T), "lse"), cache.ref,
-                                 _ints(table, q, (B, table.shape[1]), "table"), table.shape[1], _ints(lengths, q, (B,), "lengths"), st,
-                                 B, H, T, _window(window), int(sinks), float(scale), code, workspace.data_ptr(),
-                                 workspace.numel(), _stream()))
+    else:
+        n = workspace.numel()
+    st = _pack("6q", *_stride3(q, q, shape, "q"), *_stride3(out, q, shape, "out"))
+    status = load().baps_kv_attention(
+        q.data_ptr(), out.data_ptr(), lse_ptr, cache.struct, _buffer(table, torch.int32, device, (B, width), "table"), width,
+        _buffer(lengths, torch.int32, device, (B,), "lengths"), st, B, H, T, _window(window), int(sinks), float(scale), code,
+        workspace.data_ptr(), n, _stream())
+    if status:
+        _check("baps_kv_attention", status)
     return (out, lse) if want_lse else out
 
 
-def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int) -> int:
-    """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: sizes that it refuses)."""
-    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D))
-
-
-def _pages_workspace(lib, rows: int, cache: KvCache) -> torch.Tensor:
-    return torch.empty(lib.baps_kv_pages_workspace(rows, cache.k.shape[0]), dtype=torch.uint8, device=cache.k.device)
+@functools.lru_cache(maxsize=256)
+def _pages_workspace(rows: int, n_pages: int) -> int:
+    return int(load().baps_kv_pages_workspace(rows, n_pages))
 
 
 def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int = 0, window: Optional[int] = None,
                  sinks: int = 0):
     """Rebuild the rows of a batch: new row i continues old row parents[i] (outside the table: an empty row), full
     pages shared, last pages copied for all children of a parent but the first, pages outside the window let go, free pages
-    (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a row that found
-    no room has length -1."""
-    like = cache.k
-    _on(like)
+    (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a
+    row that found no room has length -1."""
+    device, i32 = cache.here(), torch.int32
     rows, width = table.shape
-    n_pages, new_rows = like.shape[0], parents.numel()
-    lib = load()
-    new = torch.empty((new_rows, width), dtype=torch.int32, device=like.device)
-    new_lengths = torch.empty(new_rows, dtype=torch.int32, device=like.device)
-    new_refs = torch.empty(n_pages, dtype=torch.int32, device=like.device)
-    ws = _pages_workspace(lib, new_rows, cache)
-    _check("baps_kv_fork",
-           lib.baps_kv_fork(cache.ref, _ints(table, like, (rows, width), "table"), _ints(lengths, like, (rows,), "lengths"), rows,
-                            _ints(refs, like, (n_pages,), "refs"), _ints(parents, like, (new_rows,), "parents"), new_rows, width,
-                            int(reserve), _window(window), int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(),
-                            ws.data_ptr(), ws.numel(), _stream()))
+    n_pages, (new_rows,) = cache.k.shape[0], parents.shape
+    ptrs = (_buffer(table, i32, device, (rows, width), "table"), _buffer(lengths, i32, device, (rows,), "lengths"),
+            _buffer(refs, i32, device, (n_pages,), "refs"), _buffer(parents, i32, device, (new_rows,), "parents"))
+    new, new_lengths, new_refs = table.new_empty((new_rows, width)), torch.empty_like(parents), torch.empty_like(refs)
+    n = _pages_workspace(new_rows, n_pages)
+    ws = cache.k.new_empty((n,))
+    status = load().baps_kv_fork(cache.struct, ptrs[0], ptrs[1], rows, ptrs[2], ptrs[3], new_rows, width, int(reserve), _window(window),
+                                 int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(), ws.data_ptr(), n, _stream())
+    if status:
+        _check("baps_kv_fork", status)
     return new, new_lengths, new_refs
 
 
 def baps_kv_compact(cache: KvCache, table, refs):
     """Move the pages in use to the front of the pool.  Returns (new_table, new_refs, page_map, n_live), all int32."""
-    like = cache.k
-    _on(like)
+    device, i32 = cache.here(), torch.int32
     rows, width = table.shape
-    n_pages = like.shape[0]
-    lib = load()
-    new = torch.empty((rows, width), dtype=torch.int32, device=like.device)
-    new_refs = torch.empty(n_pages, dtype=torch.int32, device=like.device)
-    page_map = torch.empty(n_pages, dtype=torch.int32, device=like.device)
-    n_live = torch.empty(1, dtype=torch.int32, device=like.device)
-    ws = _pages_workspace(lib, 0, cache)
-    _check("baps_kv_compact",
-           lib.baps_kv_compact(cache.ref, _ints(table, like, (rows, width), "table"), rows, width, _ints(refs, like, (n_pages,), "refs"),
-                               new.data_ptr(), new_refs.data_ptr(), page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(),
-                               ws.numel(), _stream()))
+    n_pages = cache.k.shape[0]
+    table_ptr, refs_ptr = _buffer(table, i32, device, (rows, width), "table"), _buffer(refs, i32, device, (n_pages,), "refs")
+    new, new_refs, page_map, n_live = torch.empty_like(table), torch.empty_like(refs), torch.empty_like(refs), refs.new_empty((1,))
+    n = _pages_workspace(0, n_pages)
+    ws = cache.k.new_empty((n,))
+    status = load().baps_kv_compact(cache.struct, table_ptr, rows, width, refs_ptr, new.data_ptr(), new_refs.data_ptr(),
+                                    page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(), n, _stream())
+    if status:
+        _check("baps_kv_compact", status)
     return new, new_refs, page_map, n_live

@@ -1,26 +1,28 @@
 // Attention of the last T tokens of every sequence over the 8-bit cache.
 //
 //     s = c * k_scale * (q . k_code),  w = 2^(s - m),  l = sum w,  O~ = sum w * v_scale * v_code;   O = O~ / l
-// with c = log2(e) * scale and a running maximum m that moves only when a score passes it by more than 8.  Codes become
-// fp16 in registers (exactly: E4M3 has 4 significant bits), q is scaled by a power of two per row so that its 8 or 11 bits
-// fit fp16 (what is lost is below 2^-24 of the row's largest element), and both products run on fp16 mma.sync
-// with float32 accumulation; the weights are rounded to fp16 (half a step, 2^-12) after they have been summed.  The two
-// scales are applied in float32, v_scale by keeping O~ in units of the page's scale.
+// with c = log2(e) * scale and a running reference m, six below a maximum that is followed when a score passes it by more
+// than 8, so that weights stay below 2^14.  Codes become fp16 in registers (exactly: E4M3 has 4 significant bits), q is scaled
+// by a power of two per row so that its 8 or 11 bits fit fp16 (what is lost is below 2^-25 of the row's largest element),
+// and both products run on mma.sync m16n8k16 with float32 accumulation; the weights are rounded to fp16 (half a step, 2^-12)
+// after they have been summed.  The scales are applied in float32; O~ is kept in units of a value scale that is followed
+// where a page's leaves [unit / 64, unit].
 //
-// What bounds it: the bytes of K and V, one per element.  mma.sync, not tcgen05, because the codes have to be widened in
-// registers on the way, and because 16 rows of queries (T * H / Hkv) are all there is: the products need a third of what
-// mma.sync gives at full memory rate.
+// What bounds it: the bytes of K and V, one per element.  mma.sync, not tcgen05: the codes have to be widened in registers
+// on the way, and a CTA has 8 to 64 rows of queries, where a tcgen05 tile has 128.  K and V are the operand with 16
+// rows and the queries the one with 8 columns (S^T = K Q^T, O^T = V^T P^T), so that eight query rows waste nothing: a product of 16 x 8 x 16
+// takes 8 cycles of a scheduler's tensor core and covers 256 codes.  (Queries as the 16 rows: twice the products, 4.3 TB/s on the long
+// decoding batch.  E4M3 operands, q and weights in two parts each: mma.sync m16n8k32 is carried out as fp16 products
+// with both operands widened every time, 26 cycles instead of 5 once they change, 4.6 TB/s.)
 //
 // Work is cut evenly whatever the lengths: the 64-key tiles of all sequences and kv heads, visible ones only, in one row;
 // CTA i takes an equal share.  What a CTA does of a sequence and head that is not whole goes to the workspace and a
-// second kernel joins it, in the order of the CTAs.  A tile is loaded by TMA, page by page, into a ring of stages; each
-// consumer warp takes 16-key steps of it for 16 rows and keeps m, l and O~ in registers, and the warps are joined
+// second kernel joins it, in the order of the CTAs.  A tile is loaded by TMA, page by page, into a ring of stages; a
+// consumer warp takes 32 keys of it for 8 or 16 rows and keeps m, l and O~ in registers, and the warps are joined
 // through shared memory where a sequence and head ends.
 //
-// Fragments (mma m16n8k16; g = lane / 4, t = lane % 4).  The order of the head's elements within a product and that of keys
-// within a step are free, so a thread takes whole 16-byte pieces: of K row(g) elements 16 t .. 16 t + 15 of each 64, of V
-// rows row(2 t), row(2 t + 1) elements g D / 8 .. + D / 8 - 1.  row() is chosen so that neither read of the swizzled tile
-// meets a bank twice.
+// Fragments (g = lane / 4, t = lane % 4).  The order of keys within 16 is free: place i is key key_of(i), chosen so that neither the
+// reads of K nor those of V, which ldmatrix transposes byte by byte, meet a bank twice.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -48,16 +50,21 @@ struct KvAttnParams {
 constexpr int kKvTile = 64, kKvLogTile = 6, kKvMaxB = 4096;
 constexpr int kKvMinTiles = 2;                   // tiles that a CTA takes at least
 
-template <int D, int kChunks, int kKeyGroups>
+// kTiles: groups of eight rows that a warp serves; kGroups: groups of warps with rows of their own; kTileGroups: tiles that
+// the CTA's warps work on at a time.
+template <int D, int kTiles, int kGroups, int kTileGroups>
 struct KvLayout {
-    static constexpr int kWarps = kChunks * kKeyGroups, kRows = 16 * kChunks, kThreads = kWarps * 32 + 32;
+    static constexpr int kWarps = kGroups * 2 * kTileGroups, kRows = 8 * kTiles * kGroups, kThreads = kWarps * 32 + 32;
     static constexpr int kCtasPerSm = kWarps == 4 ? 2 : 1;
     static constexpr int kTileBytes = kKvTile * D;                       // of K, and of V
     static constexpr int kStages = (kCtasPerSm == 2 ? 64 : 128) * 1024 / (2 * kTileBytes);
+    // A stage always belongs to the same warps: one that skipped a phase of its barrier could take the parity of the phase
+    // before for that of its own, pass early, and give back a tile that has not arrived.
+    static_assert(kStages % kTileGroups == 0, "a stage has to be read by the same warps in every phase");
     static constexpr int kRingOff = 0;
-    static constexpr int kJoinOff = kStages * 2 * kTileBytes;            // [warp][D / 8][lane] float4
-    static constexpr int kMlOff = kJoinOff + kWarps * 16 * D * 4;        // [warp][16] (m, l)
-    static constexpr int kMetaOff = kMlOff + kWarps * 16 * 8;            // [stage][4] (k_scale, v_scale)
+    static constexpr int kJoinOff = kStages * 2 * kTileBytes;            // [warp][kTiles][D / 8][lane] float2
+    static constexpr int kMlOff = kJoinOff + kWarps * kTiles * 8 * D * 4;    // [warp][8 kTiles] (m, l)
+    static constexpr int kMetaOff = kMlOff + kWarps * kTiles * 8 * 8;    // [stage][4] (k_scale, v_scale)
     static constexpr int kBarOff = kMetaOff + kStages * 4 * 8;
     static constexpr int kMiscOff = kBarOff + 2 * kStages * 8;
     static constexpr int kSeqOff = kMiscOff + 16;                        // int len[B], pre[B + 1]
@@ -70,7 +77,7 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// fp16 values of the two codes in the lower / upper half of a word
+// fp16 values of the two lower / upper codes of a word
 __device__ __forceinline__ uint32_t widen_lo(uint32_t x)
 {
     uint32_t d;
@@ -82,6 +89,30 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t x)
     uint32_t d;
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(d) : "r"(x));
     return d;
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// Two 16 x 16 matrices of bytes, transposed: r[2 m + h] of thread (g, t) is column 8 h + g, rows 4 t .. 4 t + 3 of matrix m.
+__device__ __forceinline__ void ldmatrix_bytes(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// 8 x 8 matrix of 16-bit elements, transposed between the threads of a warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
+}
+// Key (0 .. 15) that stands at place i of a product over 16 keys.
+__device__ __forceinline__ int key_of(int i)
+{
+    const int e0 = i & 1, e1 = (i >> 1) & 1, t0 = (i >> 2) & 1, t1 = i >> 3;
+    return t1 << 3 | t0 << 2 | e0 << 1 | (t1 ^ e1);
 }
 
 // Positions that a sequence's queries see, as 64-key tiles.
@@ -109,29 +140,23 @@ __device__ __forceinline__ KvPlace kv_place(const int *pre, int B, int heads, in
     return a;
 }
 
+// Elements d0 .. d0 + 3 of an output row from O~ and l (against m); d0 = 0 brings the lse along.
 template <typename T16>
-__device__ __forceinline__ float to_float(T16 x)
-{
-    if constexpr (__is_same(T16, __half)) return __half2float(x); else return __bfloat162float(x);
-}
-
-// Elements d0 .. d0 + 3 of an output row from O~ and l (against the maximum m); d0 = 0 brings the lse along.
-template <typename T16>
-__device__ __forceinline__ void kv_store(const KvAttnParams &p, int b, int h, int tq, int d0, float4 o, float m, float l)
+__device__ __forceinline__ void kv_store(const KvAttnParams &p, int b, int h, int tq, int d0, const float (&o)[4], float m, float l)
 {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2 *>(reinterpret_cast<T16 *>(p.out) + b * p.os_b + h * p.os_h + tq * p.os_t + d0) =
-        make_uint2(pack16<T16>(o.x * inv, o.y * inv), pack16<T16>(o.z * inv, o.w * inv));
+        make_uint2(pack16<T16>(o[0] * inv, o[1] * inv), pack16<T16>(o[2] * inv, o[3] * inv));
     if (d0 == 0 && p.lse)
         p.lse[((int64_t)b * p.H + h) * p.T + tq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
-template <typename T16, int D, int kChunks, int kKeyGroups>
-__global__ void __launch_bounds__(KvLayout<D, kChunks, kKeyGroups>::kThreads, KvLayout<D, kChunks, kKeyGroups>::kCtasPerSm)
+template <typename T16, int D, int kTiles, int kGroups, int kTileGroups>
+__global__ void __launch_bounds__(KvLayout<D, kTiles, kGroups, kTileGroups>::kThreads, KvLayout<D, kTiles, kGroups, kTileGroups>::kCtasPerSm)
 kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const KvAttnParams p)
 {
     using namespace sm100;
-    using L = KvLayout<D, kChunks, kKeyGroups>;
+    using L = KvLayout<D, kTiles, kGroups, kTileGroups>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sbase = smem_u32(smem);
@@ -143,7 +168,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 
     allow_next_kernel();
     if (tid == 0) {
-        for (int s = 0; s < L::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), L::kWarps); }
+        for (int s = 0; s < L::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 2 * kGroups); }
         mbar_fence_init();
         *s_abort = 0;
     }
@@ -238,201 +263,227 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     }
 
     // ======================= consumers =====================================================================
-    const int chunk = warp / kKeyGroups, kg = warp % kKeyGroups;
+    const int group = warp % kGroups, half = warp / kGroups % 2, tg = warp / (2 * kGroups);
     const int g = lane >> 2, t = lane & 3;
-    constexpr int kSegs = D / 64;
-    // key row of fragment index i (0 .. 7) within eight rows, see the file comment
-    auto row_of = [](int i) {
-        const int b0 = i & 1, b1 = (i >> 1) & 1, b2 = i >> 2;
-        return D == 128 ? ((b2 ^ b0) << 2) | (b1 << 1) | b0 : (b2 << 2) | (b0 << 1) | (b1 ^ b0);
-    };
-    const int kr = row_of(g), v0r = row_of(2 * t), v1r = row_of(2 * t + 1);
-    // byte offset in a swizzled tile of 16-byte part `part` of row `row`
+    // byte offset of 16-byte part `part` of row `row` in a swizzled tile
     auto at = [](int row, int part) { return (uint32_t)(row * D + ((part ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4)); };
+    // What this lane addresses of the first 16 of its warp's keys (the second 16 and other parts: plus 16 rows, exclusive or, which
+    // the swizzle lets through).  K: places of product rows 0 .. 7 and 8 .. 15, parts 0 and 1.  V: place lane % 16 of the
+    // first (lanes 0 .. 15) or second 16 keys.
+    const int pair = (lane & 7) >> 1, odd = lane & 1;
+    const uint32_t k_at = at(32 * half + key_of(4 * pair + 2 * (lane >> 3 & 1) + odd), lane >> 4);
+    const uint32_t v_at = at(32 * half + 16 * (lane >> 4) + key_of(lane & 15), 0);
+    // the thread's keys of each 16: of the scores (product rows g, g + 8), of V (places 4 t .. 4 t + 3)
+    const int s_key[2] = {32 * half + key_of(4 * (g >> 1) + (g & 1)), 32 * half + key_of(4 * (g >> 1) + 2 + (g & 1))};
 
-    int n = 0;                                                           // tiles used
+    int n = 0;                                                           // tiles behind this CTA
     for (int w = w0; w < w1;) {
         const KvPlace a = kv_place(s_pre, p.B, heads, w);
         const int tiles = min(a.n - a.i, w1 - w);
-        const int len = s_len[a.b], hk = a.hr / p.groups, row_base = (a.hr % p.groups) * L::kRows + chunk * 16;
+        const int len = s_len[a.b], hk = a.hr / p.groups, row_base = (a.hr % p.groups) * L::kRows + group * 8 * kTiles;
         const KeyTiles kt = kv_tiles(len, p.T, p.window, p.sinks);
         const int q_first = len - p.T;                                   // position of query 0, maybe below 0
 
-        // ---- the warp's 16 rows of q: row r is query r % T of head r / T of the group ---------------------
-        uint32_t qa[kSegs * 4][4];
-        float cq[2], m[2], l[2];
-        int pos[2];                                                      // of the thread's two rows; below 0: sees nothing
+        // ---- the warp's rows of q: row r is query r % T of head r / T of the group ---------------------------
+        uint32_t qb[kTiles][D / 16][2];                                  // elements 16 i + 4 t .. + 3 of row g
+        float cq[kTiles][2], m[kTiles][2], l[kTiles][2];                 // of rows 2 t, 2 t + 1
+        int pos[kTiles][2];                                              // their positions; below 0: sees nothing
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = row_base + g + 8 * half;
+        for (int qt = 0; qt < kTiles; ++qt) {
+            const int r = row_base + 8 * qt + g;
             const bool there = r < p.R;
-            const int tq = r % p.T, hq = hk * p.G + r / p.T;
-            pos[half] = there ? q_first + tq : -1;
-            float x[kSegs * 16];
-            if (there) {
-                const T16 *src = reinterpret_cast<const T16 *>(p.q) + a.b * p.qs_b + hq * p.qs_h + tq * p.qs_t + 16 * t;
+            const int tq = r % p.T;
+            float x[D / 4], big = 0.f;
+            const T16 *src = reinterpret_cast<const T16 *>(p.q) + a.b * p.qs_b + (hk * p.G + r / p.T) * p.qs_h + tq * p.qs_t + 4 * t;
 #pragma unroll
-                for (int s = 0; s < kSegs; ++s)
+            for (int i = 0; i < D / 16; ++i) {
+                uint2 u = make_uint2(0, 0);
+                if (there) u = *reinterpret_cast<const uint2 *>(src + 16 * i);
+                const float2 f0 = values2<T16>(u.x), f1 = values2<T16>(u.y);
+                x[4 * i] = f0.x; x[4 * i + 1] = f0.y; x[4 * i + 2] = f1.x; x[4 * i + 3] = f1.y;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint4 v = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * e);
-                        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 f = values2<T16>(u[k]);
-                            x[16 * s + 8 * e + 2 * k] = f.x; x[16 * s + 8 * e + 2 * k + 1] = f.y;
-                        }
-                    }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kSegs * 16; ++k) x[k] = 0.f;
+                for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(x[4 * i + k]));
             }
-            float scale = 1.f, back = 1.f;
+            float scale = 1.f, back = p.c;
             if constexpr (!__is_same(T16, __half)) {                     // largest element of the row to [1, 2)
-                float big = 0.f;
-#pragma unroll
-                for (int k = 0; k < kSegs * 16; ++k) big = fmaxf(big, fabsf(x[k]));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-                back = __uint_as_float(e << 23);
                 scale = __uint_as_float((254u - e) << 23);
+                back *= __uint_as_float(e << 23);
             }
-            cq[half] = p.c * back;
-            m[half] = -INFINITY;
-            l[half] = 0.f;
 #pragma unroll
-            for (int s = 0; s < kSegs; ++s)
+            for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {                            // product k of the segment: bytes 4 k .. 4 k + 3
-                    qa[s * 4 + k][half] = pack16<__half>(x[16 * s + 4 * k] * scale, x[16 * s + 4 * k + 1] * scale);
-                    qa[s * 4 + k][half + 2] = pack16<__half>(x[16 * s + 4 * k + 2] * scale, x[16 * s + 4 * k + 3] * scale);
-                }
+                for (int k = 0; k < 2; ++k) qb[qt][i][k] = pack16<__half>(x[4 * i + 2 * k] * scale, x[4 * i + 2 * k + 1] * scale);
+            const int here = there ? q_first + tq : -1;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                cq[qt][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t + e));
+                pos[qt][e] = __shfl_sync(0xffffffffu, here, 4 * (2 * t + e));
+                m[qt][e] = -INFINITY;
+                l[qt][e] = 0.f;
+            }
         }
-        float o[D / 8][4];
+        float o[kTiles][D / 16][4];                                      // elements 16 i + g, + 8 of rows 2 t, 2 t + 1
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
+        for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
-        float unit = 0.f;                                                // scale of the page that O~ is in units of; 0: none yet
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[qt][i][k] = 0.f;
+        float unit = 0.f;                                                // value scale that O~ is in units of; 0: none yet
+        auto times = [&](int qt, float f0, float f1) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) { o[qt][i][0] *= f0; o[qt][i][1] *= f1; o[qt][i][2] *= f0; o[qt][i][3] *= f1; }
+        };
+        auto to_unit = [&](float next) {
+            const float f = unit / next;
+#pragma unroll
+            for (int qt = 0; qt < kTiles; ++qt) times(qt, f, f);
+            unit = next;
+        };
 
         for (int i = 0; i < tiles; ++i, ++n) {
+            if (kTileGroups > 1 && n % kTileGroups != tg) continue;
             const int s = n % L::kStages;
             mbar_wait(full(s), (uint32_t)((n / L::kStages) & 1), s_abort, &g_async_status, 0x510);
             const int c0 = kt.tile(a.i + i) * kKvTile;
             // every query sees every key of the tile
             const bool all = c0 + kKvTile - 1 <= q_first && (c0 > len - 1 - p.window || c0 + kKvTile - 1 < p.sinks);
             const uint32_t ktile = sbase + L::kRingOff + s * 2 * L::kTileBytes, vtile = ktile + L::kTileBytes;
-#pragma unroll 1
-            for (int step = 0; step < 4 / kKeyGroups; ++step) {
-                const int key0 = (kg * (4 / kKeyGroups) + step) * 16;    // of the tile
-                const float2 meta = *reinterpret_cast<const float2 *>(smem + L::kMetaOff + (s * 4 + key0 / box_rows) * 8);
-                if (meta.x < 0.f) continue;                              // no such page
-                // ---- scores: two n-tiles of eight keys -------------------------------------------------------
-                float sc[2][4];
+            // scales of the two 16-key blocks; a k_scale of -1: no such page
+            const float2 *meta = reinterpret_cast<const float2 *>(smem + L::kMetaOff + s * 32);
+            const float2 sa = meta[32 * half / box_rows], sb = meta[(32 * half + 16) / box_rows];
+            const bool gone_a = sa.x == -1.f, gone_b = sb.x == -1.f;
+            if (!(gone_a && gone_b)) {
+                // ---- scores: sc[qt][block]: keys s_key[0] (rows 2 t, 2 t + 1), s_key[1] ------------------------
+                float sc[kTiles][2][4];
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
+                for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) sc[nt][k] = 0.f;
+                    for (int k = 0; k < 8; ++k) sc[qt][k >> 2][k & 3] = 0.f;
 #pragma unroll
-                    for (int seg = 0; seg < kSegs; ++seg) {
-                        const uint4 kv = lds_u32x4(ktile + at(key0 + 8 * nt + kr, 4 * seg + t));
-                        const uint32_t u[4] = {kv.x, kv.y, kv.z, kv.w};
+                for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_f16(sc[nt], qa[seg * 4 + k], widen_lo(u[k]), widen_hi(u[k]));
+                    for (int blk = 0; blk < 2; ++blk) {
+                        uint32_t u[4];                                   // parts 2 j (rows g, g + 8), 2 j + 1
+                        ldmatrix4(u, ktile + ((k_at + blk * 16 * D) ^ (uint32_t)(32 * j)));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t k16[4] = {widen_lo(u[2 * e]), widen_lo(u[2 * e + 1]), widen_hi(u[2 * e]), widen_hi(u[2 * e + 1])};
+#pragma unroll
+                            for (int qt = 0; qt < kTiles; ++qt) mma_f16(sc[qt][blk], k16, qb[qt][2 * j + e][0], qb[qt][2 * j + e][1]);
+                        }
                     }
-                }
-                // ---- s in base 2, mask ----------------------------------------------------------------------
-                bool hide[4] = {false, false, false, false};             // keys that no query sees: V may hold anything
+                // ---- s in base 2, mask -------------------------------------------------------------------------
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float f = cq[half] * meta.x;
+                for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) sc[k >> 1][2 * half + (k & 1)] *= f;
-                }
-                if (!all) {
+                    for (int e = 0; e < 2; ++e) {
+                        const float fa = cq[qt][e] * sa.x, fb = cq[qt][e] * sb.x;
+                        sc[qt][0][e] *= fa; sc[qt][0][2 + e] *= fa; sc[qt][1][e] *= fb; sc[qt][1][2 + e] *= fb;
+                    }
+                const bool part = !all || gone_a || gone_b;
+                uint32_t keep[2] = {0xffffffffu, 0xffffffffu};           // bytes of V whose keys some query sees
+                if (part) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int j = c0 + key0 + 8 * (k >> 1) + ((k & 1) ? v1r : v0r);
-                        hide[k] = j >= len || !(j > max(q_first, 0) - p.window || j < p.sinks);
+                    for (int blk = 0; blk < 2; ++blk) {
+                        const bool gone = blk ? gone_b : gone_a;
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const bool see = j <= pos[half] && (j > pos[half] - p.window || j < p.sinks);
-                            if (!see) sc[k >> 1][2 * half + (k & 1)] = -INFINITY;
+                        for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int j = c0 + 16 * blk + s_key[k >> 1], at_pos = pos[qt][k & 1];
+                                if (gone || !(j <= at_pos && (j > at_pos - p.window || j < p.sinks))) sc[qt][blk][k] = -INFINITY;
+                            }
+                        keep[blk] = 0u;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int j = c0 + 32 * half + 16 * blk + key_of(4 * t + k);
+                            if (!gone && j < len && (j > max(q_first, 0) - p.window || j < p.sinks)) keep[blk] |= 0xffu << (8 * k);
                         }
                     }
                 }
-                // ---- running maximum ------------------------------------------------------------------------
-                float mx[2];
+                // ---- running reference ---------------------------------------------------------------------------
+                float mx[kTiles][2];
+                bool rises = false;
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    mx[half] = fmaxf(fmaxf(sc[0][2 * half], sc[0][2 * half + 1]), fmaxf(sc[1][2 * half], sc[1][2 * half + 1]));
-                if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.f || mx[1] > m[1] + 8.f)) {
-                    float f[2];
+                for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 1));
-                        mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 2));
-                        const float m_new = fmaxf(m[half], mx[half]);
-                        f[half] = m[half] == -INFINITY ? 1.f : ex2_approx(m[half] - m_new);
-                        m[half] = m_new;
-                        l[half] *= f[half];
+                    for (int e = 0; e < 2; ++e) {
+                        mx[qt][e] = fmaxf(max3(sc[qt][0][e], sc[qt][0][2 + e], sc[qt][1][e]), sc[qt][1][2 + e]);
+                        rises |= mx[qt][e] > m[qt][e] + 14.f;
                     }
+                if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
-                    for (int k = 0; k < D / 8; ++k) { o[k][0] *= f[0]; o[k][1] *= f[0]; o[k][2] *= f[1]; o[k][3] *= f[1]; }
-                }
-                // ---- O~ in units of this page's value scale ---------------------------------------------------
-                float in_unit = 1.f;
-                if (meta.y != unit) {
-                    if (unit == 0.f) unit = meta.y;
-                    else if (meta.y < unit * 5.421010862427522e-20f) in_unit = 0.f;          // 2^-64: does not count
-                    else {
-                        const float f = unit / meta.y;
+                    for (int qt = 0; qt < kTiles; ++qt) {
+                        float f[2];
 #pragma unroll
-                        for (int k = 0; k < D / 8; ++k)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[k][e] *= f;
-                        unit = meta.y;
+                        for (int e = 0; e < 2; ++e) {
+                            float top = mx[qt][e];
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                            const float m_new = fmaxf(m[qt][e], top - 6.f);
+                            f[e] = m[qt][e] == -INFINITY ? 1.f : ex2_approx(m[qt][e] - m_new);
+                            m[qt][e] = m_new;
+                            l[qt][e] *= f[e];
+                        }
+                        times(qt, f[0], f[1]);
                     }
                 }
-                // ---- weights --------------------------------------------------------------------------------
-                uint32_t pa[4];
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float mu = m[half] == -INFINITY ? 0.f : m[half];
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) {
-                        const float x = ex2_approx(sc[nt][2 * half] - mu), y = ex2_approx(sc[nt][2 * half + 1] - mu);
-                        l[half] += x + y;
-                        pa[half + 2 * nt] = pack16<__half>(x * in_unit, y * in_unit);
-                    }
+                // ---- the unit of O~ ----------------------------------------------------------------------------
+                const float va = gone_a ? sb.y : sa.y, vb = gone_b ? sa.y : sb.y;
+                const float v_most = fmaxf(va, vb), v_least = fminf(va, vb);
+                if (!(v_most <= unit && v_least * 64.f >= unit)) {
+                    if (unit == 0.f) unit = v_most;
+                    else if (v_most > unit * 5.421010862427522e-20f) to_unit(v_most);        // 2^-64; below, it does not count
                 }
-                // ---- O~ += P V ------------------------------------------------------------------------------
-                constexpr int kWords = D / 32;                           // 4-byte words of a thread's part of a V row
-                uint32_t v[4][kWords];
+                // ---- weights ---------------------------------------------------------------------------------------
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = key0 + 8 * (k >> 1) + ((k & 1) ? v1r : v0r);
-                    if constexpr (D == 128) {
-                        const uint4 u = lds_u32x4(vtile + at(row, g));
-                        v[k][0] = u.x; v[k][1] = u.y; v[k][2] = u.z; v[k][3] = u.w;
-                    } else {
-                        const float2 u = lds_f32x2(vtile + at(row, g >> 1) + (g & 1) * 8);
-                        v[k][0] = __float_as_uint(u.x); v[k][1] = __float_as_uint(u.y);
+                for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float mu = m[qt][e] == -INFINITY ? 0.f : m[qt][e];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float &x = sc[qt][k >> 1][2 * (k & 1) + e];
+                            x = ex2_approx(x - mu);
+                            l[qt][e] += x;
+                        }
                     }
-                    if (!all) {
-#pragma unroll
-                        for (int e = 0; e < kWords; ++e) v[k][e] = hide[k] ? 0u : v[k][e];
+                // ---- O~ += P V: at once, or one block after the other where their scales are far apart -----------
+                const bool apart = v_least * 64.f < unit && va != vb;
+#pragma unroll 1
+                for (int pass = 0; pass < (apart ? 2 : 1); ++pass) {
+                    float fa = va / unit, fb = vb / unit;                // powers of two up to 1
+                    if (apart) {
+                        const float mine = pass ? vb : va;
+                        if (mine > unit * 5.421010862427522e-20f && mine != unit) to_unit(mine);
+                        fa = pass ? 0.f : mine / unit;
+                        fb = pass ? mine / unit : 0.f;
                     }
-                }
+                    uint32_t pb[kTiles][2][2];                           // per block: places 0 .. 7, 8 .. 15 of row g
 #pragma unroll
-                for (int e = 0; e < kWords; ++e) {
-                    const uint32_t ab = __byte_perm(v[0][e], v[1][e], 0x5140), ab2 = __byte_perm(v[0][e], v[1][e], 0x7362);
-                    const uint32_t cd = __byte_perm(v[2][e], v[3][e], 0x5140), cd2 = __byte_perm(v[2][e], v[3][e], 0x7362);
-                    mma_f16(o[4 * e], pa, widen_lo(ab), widen_lo(cd));
-                    mma_f16(o[4 * e + 1], pa, widen_hi(ab), widen_hi(cd));
-                    mma_f16(o[4 * e + 2], pa, widen_lo(ab2), widen_lo(cd2));
-                    mma_f16(o[4 * e + 3], pa, widen_hi(ab2), widen_hi(cd2));
+                    for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+                        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                pb[qt][blk][k] = transpose8(pack16<__half>(sc[qt][blk][2 * k] * (blk ? fb : fa), sc[qt][blk][2 * k + 1] * (blk ? fb : fa)));
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t u[4];                                   // per block: elements 16 c + g, 16 c + 8 + g
+                        ldmatrix_bytes(u, vtile + (v_at ^ (uint32_t)(16 * c)));
+                        if (part) { u[0] &= keep[0]; u[1] &= keep[0]; u[2] &= keep[1]; u[3] &= keep[1]; }
+#pragma unroll
+                        for (int blk = 0; blk < 2; ++blk) {
+                            const uint32_t v16[4] = {widen_lo(u[2 * blk]), widen_lo(u[2 * blk + 1]), widen_hi(u[2 * blk]), widen_hi(u[2 * blk + 1])};
+#pragma unroll
+                            for (int qt = 0; qt < kTiles; ++qt) mma_f16(o[qt][c], v16, pb[qt][blk][0], pb[qt][blk][1]);
+                        }
+                    }
                 }
             }
             __syncwarp();
@@ -440,55 +491,52 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         }
 
         // ---- join the warps that share these rows ----------------------------------------------------------
-        float4 *join = reinterpret_cast<float4 *>(smem + L::kJoinOff);
+        float2 *join = reinterpret_cast<float2 *>(smem + L::kJoinOff);
         float2 *ml = reinterpret_cast<float2 *>(smem + L::kMlOff);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
-            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
-            if (t == 0) ml[warp * 16 + g + 8 * half] = make_float2(m[half], l[half]);
-        }
-        // thread (g, t) holds elements (2 t) D / 8 + i and (2 t + 1) D / 8 + i, i = 0 .. D / 8 - 1, of rows g and g + 8:
-        // slot (half, e, quarter) is elements (2 t + e) D / 8 + 4 quarter .. + 3 of row g + 8 half
+        for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+            for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+                for (int x = 4; x < 32; x <<= 1) l[qt][e] += __shfl_xor_sync(0xffffffffu, l[qt][e], x);
+                if (g == 0) ml[warp * 8 * kTiles + 8 * qt + 2 * t + e] = make_float2(m[qt][e], l[qt][e]);
+            }
 #pragma unroll
-                for (int qr = 0; qr < D / 32; ++qr)
-                    join[(warp * (D / 8) + (half * 2 + e) * (D / 32) + qr) * 32 + lane] =
-                        make_float4(o[4 * qr][2 * half + e] * unit, o[4 * qr + 1][2 * half + e] * unit,
-                                    o[4 * qr + 2][2 * half + e] * unit, o[4 * qr + 3][2 * half + e] * unit);
+        for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k)                              // element 8 k + g of rows 2 t, 2 t + 1
+                join[((warp * kTiles + qt) * (D / 8) + k) * 32 + lane] =
+                    make_float2(o[qt][k >> 1][2 * (k & 1)] * unit, o[qt][k >> 1][2 * (k & 1) + 1] * unit);
         named_bar_sync(1, L::kWarps * 32);
         const bool whole = tiles == a.n;
-        const bool good = *s_abort == 0;
-        const int slot = 2 * blockIdx.x + (a.i == 0 ? 1 : 0);
-        // the chunk's kKeyGroups warps share its D / 8 slots of 32 lanes
-        for (int sl = kg; good && sl < D / 8; sl += kKeyGroups) {
-            const int half = sl / (2 * (D / 32)), e = sl / (D / 32) % 2, qr = sl % (D / 32);
-            const int rr = g + 8 * half, r = row_base + rr;
-            if (r >= p.R) continue;
-            float M = -INFINITY, Lsum = 0.f;
-            float2 part[kKeyGroups];
+        constexpr int kSame = 2 * kTileGroups;                           // warps with the same rows: group, group + kGroups, ...
+        if (*s_abort == 0)
+            for (int x = (warp / kGroups) * 32 + lane; x < 8 * kTiles * (D / 4); x += kSame * 32) {
+                const int rr = x / (D / 4), d0 = x % (D / 4) * 4, r = row_base + rr;
+                if (r >= p.R) continue;
+                float M = -INFINITY, Lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int x = 0; x < kKeyGroups; ++x) { part[x] = ml[(chunk * kKeyGroups + x) * 16 + rr]; M = fmaxf(M, part[x].x); }
-            const float Mu = M == -INFINITY ? 0.f : M;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int y = 0; y < kSame; ++y) M = fmaxf(M, ml[(group + y * kGroups) * 8 * kTiles + rr].x);
+                const float Mu = M == -INFINITY ? 0.f : M;
 #pragma unroll
-            for (int x = 0; x < kKeyGroups; ++x) {
-                const float f = ex2_approx(part[x].x - Mu);
-                const float4 u = join[((chunk * kKeyGroups + x) * (D / 8) + sl) * 32 + lane];
-                Lsum += f * part[x].y;
-                acc.x += f * u.x; acc.y += f * u.y; acc.z += f * u.z; acc.w += f * u.w;
+                for (int y = 0; y < kSame; ++y) {
+                    const int from = group + y * kGroups;
+                    const float2 own = ml[from * 8 * kTiles + rr];
+                    const float f = ex2_approx(own.x - Mu);
+                    Lsum += f * own.y;
+                    const float *src = reinterpret_cast<const float *>(join + ((from * kTiles + (rr >> 3)) * (D / 8) + (d0 >> 3)) * 32) +
+                                       ((d0 & 7) * 4 + (rr & 7) / 2) * 2 + (rr & 1);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[k] += f * src[8 * k];
+                }
+                if (whole) {
+                    kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
+                } else {
+                    const int64_t row = (int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + group * 8 * kTiles + rr;
+                    *reinterpret_cast<float4 *>(p.part_o + row * D + d0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                    if (d0 == 0) p.part_ml[row] = make_float2(M, Lsum);
+                }
             }
-            const int d0 = (2 * t + e) * (D / 8) + 4 * qr;
-            if (whole) {
-                kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
-            } else {
-                *reinterpret_cast<float4 *>(p.part_o + ((int64_t)slot * L::kRows + chunk * 16 + rr) * D + d0) = acc;
-                if (d0 == 0) p.part_ml[(int64_t)slot * L::kRows + chunk * 16 + rr] = make_float2(M, Lsum);
-            }
-        }
         if (tid == 0 && a.i == 0 && !whole) p.desc[blockIdx.x] = make_int2(a.b * heads + a.hr, (w + a.n - 1) / per);
         named_bar_sync(1, L::kWarps * 32);                               // before the buffers are written again
         w += tiles;
@@ -514,57 +562,58 @@ kv_join_kernel(const KvAttnParams p)
     float m = -INFINITY, l = 0.f;
     for (int k = 0; k < parts; ++k) m = fmaxf(m, p.part_ml[row(k)].x);
     const float mu = m == -INFINITY ? 0.f : m;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < parts; ++k) {
         const float2 ml = p.part_ml[row(k)];
         const float4 u = *reinterpret_cast<const float4 *>(p.part_o + row(k) * D + d0);
         const float f = ex2_approx(ml.x - mu);
         l += f * ml.y;
-        o.x += f * u.x; o.y += f * u.y; o.z += f * u.z; o.w += f * u.w;
+        o[0] += f * u.x; o[1] += f * u.y; o[2] += f * u.z; o[3] += f * u.w;
     }
     kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, d0, o, m, l);
 }
 
-// Rows of a kv head go to a CTA 16, 32 or 64 at a time, so that its K and V are read once wherever that can be: 16 rows take four
-// warps (two CTAs per SM), more take eight that read every tile once per 16 rows.
-struct KvShape { int chunks, groups, ctas; };
+// Rows of a kv head go to a CTA 8, 16, 32 or 64 at a time, so that its K and V are read once wherever that can be.  A warp serves
+// 8 or 16 of them, so up to 16 a tile is widened once; 32 rows take two groups of warps, 64 four (one CTA per SM).
+struct KvShape { int rows, groups, ctas; };
 static inline KvShape kv_shape(int R)
 {
     KvShape s;
-    s.chunks = R <= 16 ? 1 : R <= 32 ? 2 : 4;
-    s.groups = (R + 16 * s.chunks - 1) / (16 * s.chunks);
-    s.ctas = num_sms() * (s.chunks == 1 ? 2 : 1);
+    s.rows = R <= 8 ? 8 : R <= 16 ? 16 : R <= 32 ? 32 : 64;
+    s.groups = (R + s.rows - 1) / s.rows;
+    s.ctas = num_sms() * (s.rows < 64 ? 2 : 1);
     return s;
 }
 // Bytes: part_o, part_ml, desc
 static inline size_t kv_workspace(const KvShape &s, int D)
 {
-    const size_t rows = (size_t)s.ctas * 2 * 16 * s.chunks;
+    const size_t rows = (size_t)s.ctas * 2 * s.rows;
     return rows * D * 4 + rows * 8 + (size_t)s.ctas * 8;
 }
 
-template <typename T16, int D, int kChunks, int kKeyGroups>
+template <typename T16, int D, int kTiles, int kGroups, int kTileGroups>
 static inline baps_status kv_attention_launch(const CUtensorMap &mk, const CUtensorMap &mv, const KvAttnParams &p, int ctas,
                                               cudaStream_t stream)
 {
-    using L = KvLayout<D, kChunks, kKeyGroups>;
-    if (cudaFuncSetAttribute(kv_attention_kernel<T16, D, kChunks, kKeyGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    using L = KvLayout<D, kTiles, kGroups, kTileGroups>;
+    if (cudaFuncSetAttribute(kv_attention_kernel<T16, D, kTiles, kGroups, kTileGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              L::dyn_bytes(kKvMaxB)) != cudaSuccess)
         return BAPS_ERR_CUDA;
-    const baps_status s = launch_kernel(kv_attention_kernel<T16, D, kChunks, kKeyGroups>, (unsigned)ctas, L::kThreads,
+    const baps_status s = launch_kernel(kv_attention_kernel<T16, D, kTiles, kGroups, kTileGroups>, (unsigned)ctas, L::kThreads,
                                         (size_t)L::dyn_bytes(p.B), stream, mk, mv, p);
     if (s != BAPS_OK) return s;
-    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)ctas, (unsigned)(L::kRows * D / 512)), 128, 0, stream, p);
+    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)ctas, (unsigned)((L::kRows * D + 511) / 512)), 128, 0, stream, p);
 }
 
 template <typename T16, int D>
 static inline baps_status kv_attention_rows(const CUtensorMap &mk, const CUtensorMap &mv, const KvAttnParams &p,
                                             const KvShape &s, cudaStream_t stream)
 {
-    if (s.chunks == 1) return kv_attention_launch<T16, D, 1, 4>(mk, mv, p, s.ctas, stream);
-    if (s.chunks == 2) return kv_attention_launch<T16, D, 2, 4>(mk, mv, p, s.ctas, stream);
-    return kv_attention_launch<T16, D, 4, 2>(mk, mv, p, s.ctas, stream);
+    if (s.rows == 8) return kv_attention_launch<T16, D, 1, 1, 2>(mk, mv, p, s.ctas, stream);
+    if (s.rows == 16) return kv_attention_launch<T16, D, 2, 1, 2>(mk, mv, p, s.ctas, stream);
+    if (s.rows == 32) return kv_attention_launch<T16, D, 2, 2, 1>(mk, mv, p, s.ctas, stream);
+    return kv_attention_launch<T16, D, 2, 4, 1>(mk, mv, p, s.ctas, stream);
 }
 
 } // namespace baps

@@ -165,7 +165,7 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
     p.width = table_width; p.B = B; p.H = H; p.Hkv = cache->Hkv; p.T = T; p.G = H / cache->Hkv; p.R = T * p.G; p.groups = shape.groups;
     p.n_pages = cache->n_pages; p.page = cache->page; p.window = window; p.sinks = sinks;
     p.c = base2_scale(scale, D);
-    const size_t part_rows = (size_t)shape.ctas * 2 * 16 * shape.chunks;
+    const size_t part_rows = (size_t)shape.ctas * 2 * shape.rows;
     p.part_o = static_cast<float *>(workspace);
     p.part_ml = reinterpret_cast<float2 *>(p.part_o + part_rows * D);
     p.desc = reinterpret_cast<int2 *>(p.part_ml + part_rows);

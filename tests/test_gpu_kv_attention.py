@@ -1,7 +1,7 @@
 """baps_kv_attention against the definition evaluated in float64 on the CPU.
 
 Tolerances (relative to the largest |v| of a head, since an output is a mean of values): the weights are rounded to fp16,
-half a step 2^-12 each and in the same proportion as much of their sum, that is 2^-12 |v| at most; the output is
+half a step 2^-12 of each, which moves the mean by 2^-12 |v| at most (those below 2^-20 by as little); the output is
 rounded to its type, 2^-8 (bf16) or 2^-11 (fp16) of its value at most.  float32 scores of D products are off by
 (D + 4) 2^-24 of the sum of their magnitudes at most, which for the inputs below (|q . k| terms summing to under 64 in the
 exponent) is 2^-11 of a weight; ex2.approx adds 2^-22.  lse: the same 2^-11, absolute, and 2^-22 of its value."""

@@ -1,5 +1,6 @@
 """Argument checks of the serving entry points, which need no device, and the sizes of their workspaces."""
 import ctypes
+import struct
 
 import pytest
 
@@ -33,10 +34,9 @@ def test_window(lib):
 
 
 def cache(k=P, v=P, ks=P, vs=P, n_pages=8, Hkv=2, page=16, D=64):
-    return ctypes.addressof(cache.keep.setdefault((k, v, ks, vs, n_pages, Hkv, page, D), binding._Cache(k, v, ks, vs, n_pages, Hkv, page, D)))
+    return struct.pack("4Q4i", *(x or 0 for x in (k, v, ks, vs)), n_pages, Hkv, page, D)
 
 
-cache.keep = {}
 BAD_CACHES = [(-1, dict(k=None)), (-1, dict(vs=None)), (-1, dict(n_pages=0)), (-1, dict(Hkv=0)), (-2, dict(page=48)), (-2, dict(D=96)),
               (-2, dict(n_pages=1 << 30)), (-3, dict(v=BAD)), (-3, dict(ks=2))]
 
