@@ -17,9 +17,12 @@
 //
 // Work is cut evenly whatever the lengths: the 64-key tiles of all sequences and kv heads, visible ones only, in one row;
 // CTA i takes an equal share.  What a CTA does of a sequence and head that is not whole goes to the workspace and a
-// second kernel joins it, in the order of the CTAs.  A tile is loaded by TMA, page by page, into a ring of stages; a
-// consumer warp takes 32 keys of it for 8 or 16 rows and keeps m, l and O~ in registers, and the warps are joined
-// through shared memory where a sequence and head ends.
+// second kernel joins it, in the order of the CTAs.  Each of a CTA's four warps takes every fourth 32 keys of its share for 8 to 32
+// rows of queries and keeps m, l and O~ in registers; they are joined through shared memory where a sequence and head
+// ends.  A warp copies its own keys (16 bytes per lane, two to four steps ahead), so that no warp waits for another before that.
+// (Before: a producer warp and TMA boxes into a ring of tiles.  The same 6.5 TB/s for pages of 64 tokens, but a box takes
+// about 120 cycles of the SM's unit however small it is, 414 us for 309 with pages of 16; and a fifth warp costs a fifth of
+// the registers.)
 //
 // Fragments (g = lane / 4, t = lane % 4).  The order of keys within 16 is free: place i is key key_of(i), chosen so that neither the
 // reads of K nor those of V, which ldmatrix transposes byte by byte, meet a bank twice.
@@ -37,6 +40,7 @@ struct KvAttnParams {
     float *lse;
     int64_t qs_b, qs_h, qs_t, os_b, os_h, os_t;
     const int32_t *table, *lengths;
+    const uint8_t *k, *v;
     const float *k_scale, *v_scale;
     int width, B, H, Hkv, T, G, R, groups;      // G = H / Hkv, R = T * G rows per kv head, in `groups` groups of kRows
     int n_pages, page, window, sinks;
@@ -47,28 +51,25 @@ struct KvAttnParams {
     int2 *desc;                                  // (item, last CTA that has part of it); item -1: none begins here and goes on
 };
 
-constexpr int kKvTile = 64, kKvLogTile = 6, kKvMaxB = 4096;
+constexpr int kKvTile = 64, kKvLogTile = 6, kKvStep = 32, kKvMaxB = 4096;
 constexpr int kKvMinTiles = 2;                   // tiles that a CTA takes at least
 
-// kTiles: groups of eight rows that a warp serves; kGroups: groups of warps with rows of their own; kTileGroups: tiles that
-// the CTA's warps work on at a time.
-template <int D, int kTiles, int kGroups, int kTileGroups>
+// kTiles: groups of eight rows that a CTA serves.
+template <int D, int kTiles>
 struct KvLayout {
-    static constexpr int kWarps = kGroups * 2 * kTileGroups, kRows = 8 * kTiles * kGroups, kThreads = kWarps * 32 + 32;
-    static constexpr int kCtasPerSm = kWarps == 4 ? 2 : 1;
-    static constexpr int kTileBytes = kKvTile * D;                       // of K, and of V
-    static constexpr int kStages = (kCtasPerSm == 2 ? 64 : 128) * 1024 / (2 * kTileBytes);
-    // A stage always belongs to the same warps: one that skipped a phase of its barrier could take the parity of the phase
-    // before for that of its own, pass early, and give back a tile that has not arrived.
-    static_assert(kStages % kTileGroups == 0, "a stage has to be read by the same warps in every phase");
-    static constexpr int kRingOff = 0;
-    static constexpr int kJoinOff = kStages * 2 * kTileBytes;            // [warp][kTiles][D / 8][lane] float2
+    static constexpr int kWarps = 4, kThreads = 128, kRows = 8 * kTiles;
+    static constexpr int kCtasPerSm = D == 64 && kTiles < 4 ? 3 : 2;
+    static constexpr int kSlotBytes = 2 * kKvStep * D;                   // K and V of a step
+    static constexpr int kSlots = D == 64 ? (kTiles == 2 ? 3 : 4) : 2;
+    static constexpr int kSlotOff = 0;                                   // [warp][slot]
+    static constexpr int kJoinOff = kWarps * kSlots * kSlotBytes;        // [warp][kTiles][D / 8][lane] float2
     static constexpr int kMlOff = kJoinOff + kWarps * kTiles * 8 * D * 4;    // [warp][8 kTiles] (m, l)
-    static constexpr int kMetaOff = kMlOff + kWarps * kTiles * 8 * 8;    // [stage][4] (k_scale, v_scale)
-    static constexpr int kBarOff = kMetaOff + kStages * 4 * 8;
-    static constexpr int kMiscOff = kBarOff + 2 * kStages * 8;
-    static constexpr int kSeqOff = kMiscOff + 16;                        // int len[B], pre[B + 1]
-    static int dyn_bytes(int B) { return kSeqOff + (2 * B + 1) * 4 + 1024; }
+    static constexpr int kQOff = kMlOff + kWarps * kTiles * 8 * 8;       // [kTiles][D / 16][lane] uint2
+    static constexpr int kMetaOff = kQOff + kTiles * 8 * D * 2;          // [warp][slot] float4: k_scale, v_scale of both 16-key blocks
+    static constexpr int kSeqOff = kMetaOff + kWarps * kSlots * 16;      // int len[B], pre[B + 1]
+    static constexpr int dyn_bytes(int B) { return kSeqOff + (2 * B + 1) * 4; }
+    static_assert(dyn_bytes(kKvMaxB) <= 227 * 1024, "shared memory of a CTA");
+    static_assert(kCtasPerSm * (dyn_bytes(64) + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -101,6 +102,13 @@ __device__ __forceinline__ void ldmatrix_bytes(uint32_t (&r)[4], uint32_t addr)
     asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kMayBeOpen>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kMayBeOpen) : "memory"); }
 // 8 x 8 matrix of 16-bit elements, transposed between the threads of a warp
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -151,27 +159,18 @@ __device__ __forceinline__ void kv_store(const KvAttnParams &p, int b, int h, in
         p.lse[((int64_t)b * p.H + h) * p.T + tq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
-template <typename T16, int D, int kTiles, int kGroups, int kTileGroups>
-__global__ void __launch_bounds__(KvLayout<D, kTiles, kGroups, kTileGroups>::kThreads, KvLayout<D, kTiles, kGroups, kTileGroups>::kCtasPerSm)
-kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const KvAttnParams p)
+template <typename T16, int D, int kTiles>
+__global__ void __launch_bounds__(KvLayout<D, kTiles>::kThreads, KvLayout<D, kTiles>::kCtasPerSm)
+kv_attention_kernel(const KvAttnParams p)
 {
     using namespace sm100;
-    using L = KvLayout<D, kTiles, kGroups, kTileGroups>;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    using L = KvLayout<D, kTiles>;
+    extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
-    auto full = [&](int s) { return sbase + L::kBarOff + 8u * (uint32_t)s; };
-    auto empty = [&](int s) { return sbase + L::kBarOff + 8u * (uint32_t)(L::kStages + s); };
-    volatile int *s_abort = reinterpret_cast<volatile int *>(smem + L::kMiscOff);
     int *s_len = reinterpret_cast<int *>(smem + L::kSeqOff), *s_pre = s_len + p.B;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     allow_next_kernel();
-    if (tid == 0) {
-        for (int s = 0; s < L::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 2 * kGroups); }
-        mbar_fence_init();
-        *s_abort = 0;
-    }
     await_previous_kernel();
     // ---- every CTA's share: tiles of each sequence, their running sum ---------------------------------
     const int64_t most = (int64_t)p.width * p.page;
@@ -202,90 +201,92 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     const int w0 = (int)min((int64_t)blockIdx.x * per, (int64_t)total), w1 = min(w0 + per, total);
     if (tid == 0) p.desc[blockIdx.x] = make_int2(-1, 0);
     if (w0 >= w1) return;
-    constexpr int kBoxRowsMax = kKvTile;
-    const int box_rows = min(p.page, kBoxRowsMax), boxes = kKvTile / box_rows;
 
-    if (warp == L::kWarps) {
-        // ======================= producer: a lane per page box of the next 32 ============================
-        const int per_batch = 32 / boxes;
-        struct Box { int y; float ks, vs; };
-        auto fetch = [&](int w) {
-            Box x{-1, -1.f, 0.f};
-            const int mine = w + lane / boxes;
-            if (mine < w1) {
-                const KvPlace a = kv_place(s_pre, p.B, heads, mine);
-                const int len = s_len[a.b];
-                const int pos = kv_tiles(len, p.T, p.window, p.sinks).tile(a.i) * kKvTile + (lane % boxes) * box_rows;
-                if (pos < len) {
-                    const int id = p.table[(int64_t)a.b * p.width + pos / p.page];
-                    if (id >= 0 && id < p.n_pages) {
-                        const int64_t ph = (int64_t)id * p.Hkv + a.hr / p.groups;
-                        x.y = (int)(ph * p.page + pos % p.page);
-                        x.ks = p.k_scale[ph];
-                        x.vs = p.v_scale[ph];
-                    }
+    // ---- the warp's steps: number k is half (u & 1) of tile w0 + (u >> 1), u = warp + 4 k ---------------
+    // What lane l knows of step k0 + l, 32 steps at a time, the next 32 on their way: rows of the pool's [n_pages * Hkv * page, D]
+    // view where its two 16-key blocks begin (-1: no page, or no key that a query sees), their scales.
+    struct Ahead { int row_a, row_b; float ka, va, kb, vb; };
+    const int steps = w1 - w0 > warp / 2 ? (2 * (w1 - w0) - warp + 3) / 4 : 0;
+    auto fetch = [&](int k0) {
+        Ahead x{-1, -1, -1.f, 0.f, -1.f, 0.f};
+        const int k = k0 + lane;
+        if (k < steps) {
+            const int u = warp + 4 * k;
+            const KvPlace a = kv_place(s_pre, p.B, heads, w0 + (u >> 1));
+            const int len = s_len[a.b], first = max(len - p.T, 0), hk = a.hr / p.groups;
+            const int pos = kv_tiles(len, p.T, p.window, p.sinks).tile(a.i) * kKvTile + (u & 1) * kKvStep;
+            auto block = [&](int at, int &row, float &ks, float &vs) {
+                if (at >= len || !(at + 15 > first - p.window || at < p.sinks)) return;
+                const int id = p.table[(int64_t)a.b * p.width + at / p.page];
+                if (id < 0 || id >= p.n_pages) return;
+                const int64_t ph = (int64_t)id * p.Hkv + hk;
+                row = (int)(ph * p.page + at % p.page);
+                ks = p.k_scale[ph];
+                vs = p.v_scale[ph];
+            };
+            block(pos, x.row_a, x.ka, x.va);
+            block(pos + 16, x.row_b, x.kb, x.vb);
+        }
+        return x;
+    };
+    const uint32_t slots = sbase + L::kSlotOff + (uint32_t)(warp * L::kSlots * L::kSlotBytes);
+    const uint32_t metas = sbase + L::kMetaOff + (uint32_t)(warp * L::kSlots * 16);
+    // byte offset of 16-byte part `part` of row `row`: parts of neighbouring rows change places, so that eight rows' parts
+    // of one number stand in different banks
+    auto place = [](int row, int part) { return (uint32_t)(row * D + ((part ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4)); };
+    constexpr int kParts = D / 16, kRowsAtOnce = 32 / kParts;
+    const int c_row = lane / kParts, c_part = lane % kParts;
+    Ahead now = fetch(0), next = steps > 32 ? fetch(32) : now;
+    int next_k = 0, next_slot = 0;                                       // the step to be copied next, and where to
+    auto copy_step = [&] {
+        if (next_k < steps) {
+            if (next_k > 0 && (next_k & 31) == 0) { now = next; next = next_k + 32 < steps ? fetch(next_k + 32) : now; }
+            const int row_a = __shfl_sync(0xffffffffu, now.row_a, next_k & 31), row_b = __shfl_sync(0xffffffffu, now.row_b, next_k & 31);
+            const uint32_t to = slots + (uint32_t)(next_slot * L::kSlotBytes);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                const int row = blk ? row_b : row_a;
+                if (row < 0) continue;
+                const int64_t from = (int64_t)(row + c_row) * D + c_part * 16;
+                const uint8_t *k = p.k + from, *v = p.v + from;
+#pragma unroll
+                for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
+                    const uint32_t at = to + place(16 * blk + r0 + c_row, c_part);
+                    copy16(at, k + r0 * D);
+                    copy16(at + kKvStep * D, v + r0 * D);
                 }
             }
-            return x;
-        };
-        Box now = fetch(w0);
-        int n = 0;                                                       // tiles issued
-        bool ok = true;
-        for (int w = w0; ok && w < w1; w += per_batch) {
-            const Box next = w + per_batch < w1 ? fetch(w + per_batch) : now;
-            for (int k = 0; k < per_batch && w + k < w1; ++k, ++n) {
-                const int s = n % L::kStages;
-                ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)((n / L::kStages) & 1) ^ 1u, s_abort, &g_async_status, 0x500));
-                if (!ok) break;
-                const bool mine = lane / boxes == k;
-                const unsigned there = __ballot_sync(0xffffffffu, mine && now.y >= 0);
-                if (mine)
-                    *reinterpret_cast<float2 *>(smem + L::kMetaOff + (s * 4 + lane % boxes) * 8) = make_float2(now.ks, now.vs);
-                __syncwarp();
-                if (lane == 0) mbar_arrive_expect_tx(full(s), (uint32_t)(__popc(there) * 2 * box_rows * D));
-                __syncwarp();
-                if (mine && now.y >= 0) {
-                    const uint32_t at = sbase + L::kRingOff + s * 2 * L::kTileBytes + (lane % boxes) * box_rows * D;
-                    tma_load_2d(at, &mk, 0, now.y, full(s));
-                    tma_load_2d(at + L::kTileBytes, &mv, 0, now.y, full(s));
-                }
-            }
-            now = next;
+            float4 scales;                                               // k_scale -1: no such block
+            scales.x = __shfl_sync(0xffffffffu, now.ka, next_k & 31); scales.y = __shfl_sync(0xffffffffu, now.va, next_k & 31);
+            scales.z = __shfl_sync(0xffffffffu, now.kb, next_k & 31); scales.w = __shfl_sync(0xffffffffu, now.vb, next_k & 31);
+            if (lane == 0) sts_f32x4(metas + 16u * (uint32_t)next_slot, scales);
         }
-        if (*s_abort) {
-            // copies in flight land before the CTA's shared memory is released
-            for (int l = n > L::kStages ? n - L::kStages : 0; l < n; ++l) {
-                const uint64_t t0 = globaltimer_ns();
-                while (!mbar_try_wait(full(l % L::kStages), (uint32_t)((l / L::kStages) & 1)) && globaltimer_ns() - t0 < 2000000ull) {}
-            }
-        }
-        return;
-    }
+        copies_commit();                                                 // (a group for every step, also behind the last)
+        ++next_k;
+        next_slot = next_slot + 1 < L::kSlots ? next_slot + 1 : 0;
+    };
+    for (int i = 0; i < L::kSlots; ++i) copy_step();
 
-    // ======================= consumers =====================================================================
-    const int group = warp % kGroups, half = warp / kGroups % 2, tg = warp / (2 * kGroups);
     const int g = lane >> 2, t = lane & 3;
-    // byte offset of 16-byte part `part` of row `row` in a swizzled tile
-    auto at = [](int row, int part) { return (uint32_t)(row * D + ((part ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4)); };
-    // What this lane addresses of the first 16 of its warp's keys (the second 16 and other parts: plus 16 rows, exclusive or, which
-    // the swizzle lets through).  K: places of product rows 0 .. 7 and 8 .. 15, parts 0 and 1.  V: place lane % 16 of the
-    // first (lanes 0 .. 15) or second 16 keys.
-    const int pair = (lane & 7) >> 1, odd = lane & 1;
-    const uint32_t k_at = at(32 * half + key_of(4 * pair + 2 * (lane >> 3 & 1) + odd), lane >> 4);
-    const uint32_t v_at = at(32 * half + 16 * (lane >> 4) + key_of(lane & 15), 0);
+    // What this lane addresses of the first 16 keys of a step (the second 16 and other parts: plus 16 rows, exclusive or, which
+    // the order of parts lets through).  K: places of product rows 0 .. 7 and 8 .. 15, parts 0 and 1.  V: place lane % 16 of
+    // the first (lanes 0 .. 15) or second 16 keys.
+    const uint32_t k_at = place(key_of(4 * ((lane & 7) >> 1) + 2 * (lane >> 3 & 1) + (lane & 1)), lane >> 4);
+    const uint32_t v_at = kKvStep * D + place(16 * (lane >> 4) + key_of(lane & 15), 0);
     // the thread's keys of each 16: of the scores (product rows g, g + 8), of V (places 4 t .. 4 t + 3)
-    const int s_key[2] = {32 * half + key_of(4 * (g >> 1) + (g & 1)), 32 * half + key_of(4 * (g >> 1) + 2 + (g & 1))};
+    const int s_key[2] = {key_of(4 * (g >> 1) + (g & 1)), key_of(4 * (g >> 1) + 2 + (g & 1))};
+    const uint32_t q_at = sbase + L::kQOff + (uint32_t)(lane * 8);
 
-    int n = 0;                                                           // tiles behind this CTA
+    int step = 0, slot = 0;
     for (int w = w0; w < w1;) {
         const KvPlace a = kv_place(s_pre, p.B, heads, w);
         const int tiles = min(a.n - a.i, w1 - w);
-        const int len = s_len[a.b], hk = a.hr / p.groups, row_base = (a.hr % p.groups) * L::kRows + group * 8 * kTiles;
+        const int len = s_len[a.b], hk = a.hr / p.groups, row_base = (a.hr % p.groups) * L::kRows;
         const KeyTiles kt = kv_tiles(len, p.T, p.window, p.sinks);
         const int q_first = len - p.T;                                   // position of query 0, maybe below 0
+        const int steps_here = 2 * (w + tiles - w0);                     // u below this: of this sequence and head
 
-        // ---- the warp's rows of q: row r is query r % T of head r / T of the group ---------------------------
-        uint32_t qb[kTiles][D / 16][2];                                  // elements 16 i + 4 t .. + 3 of row g
+        // ---- the rows of q: row r is query r % T of head r / T of the group ------------------------------------
         float cq[kTiles][2], m[kTiles][2], l[kTiles][2];                 // of rows 2 t, 2 t + 1
         int pos[kTiles][2];                                              // their positions; below 0: sees nothing
 #pragma unroll
@@ -312,10 +313,11 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                 scale = __uint_as_float((254u - e) << 23);
                 back *= __uint_as_float(e << 23);
             }
+            // elements 16 i + 4 t .. + 3 of row g (all four warps write the same)
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) qb[qt][i][k] = pack16<__half>(x[4 * i + 2 * k] * scale, x[4 * i + 2 * k + 1] * scale);
+                sts_u32x2(q_at + (uint32_t)((qt * (D / 16) + i) * 256), pack16<__half>(x[4 * i] * scale, x[4 * i + 1] * scale),
+                          pack16<__half>(x[4 * i + 2] * scale, x[4 * i + 3] * scale));
             const int here = there ? q_first + tq : -1;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -325,6 +327,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                 l[qt][e] = 0.f;
             }
         }
+        __syncwarp();
         float o[kTiles][D / 16][4];                                      // elements 16 i + g, + 8 of rows 2 t, 2 t + 1
 #pragma unroll
         for (int qt = 0; qt < kTiles; ++qt)
@@ -332,29 +335,29 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[qt][i][k] = 0.f;
-        float unit = 0.f;                                                // value scale that O~ is in units of; 0: none yet
+        float unit = 0.f, inv_unit = 0.f;                                // value scale that O~ is in units of; 0: none yet
         auto times = [&](int qt, float f0, float f1) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) { o[qt][i][0] *= f0; o[qt][i][1] *= f1; o[qt][i][2] *= f0; o[qt][i][3] *= f1; }
         };
         auto to_unit = [&](float next) {
-            const float f = unit / next;
+            inv_unit = pow2_inverse(next);
+            const float f = unit * inv_unit;
 #pragma unroll
             for (int qt = 0; qt < kTiles; ++qt) times(qt, f, f);
             unit = next;
         };
 
-        for (int i = 0; i < tiles; ++i, ++n) {
-            if (kTileGroups > 1 && n % kTileGroups != tg) continue;
-            const int s = n % L::kStages;
-            mbar_wait(full(s), (uint32_t)((n / L::kStages) & 1), s_abort, &g_async_status, 0x510);
-            const int c0 = kt.tile(a.i + i) * kKvTile;
-            // every query sees every key of the tile
-            const bool all = c0 + kKvTile - 1 <= q_first && (c0 > len - 1 - p.window || c0 + kKvTile - 1 < p.sinks);
-            const uint32_t ktile = sbase + L::kRingOff + s * 2 * L::kTileBytes, vtile = ktile + L::kTileBytes;
-            // scales of the two 16-key blocks; a k_scale of -1: no such page
-            const float2 *meta = reinterpret_cast<const float2 *>(smem + L::kMetaOff + s * 32);
-            const float2 sa = meta[32 * half / box_rows], sb = meta[(32 * half + 16) / box_rows];
+        for (; warp + 4 * step < steps_here; ++step) {
+            copies_wait<L::kSlots - 1>();
+            __syncwarp();                                                // what the other lanes copied is there too
+            const int u = warp + 4 * step;
+            const int c0 = kt.tile(a.i + (w0 + (u >> 1) - w)) * kKvTile + (u & 1) * kKvStep;
+            // every query sees every key of the step
+            const bool all = c0 + kKvStep - 1 <= q_first && (c0 > len - 1 - p.window || c0 + kKvStep - 1 < p.sinks);
+            const uint32_t base = slots + (uint32_t)(slot * L::kSlotBytes);
+            const float4 scales = lds_f32x4(metas + 16u * (uint32_t)slot);
+            const float2 sa = make_float2(scales.x, scales.y), sb = make_float2(scales.z, scales.w);
             const bool gone_a = sa.x == -1.f, gone_b = sb.x == -1.f;
             if (!(gone_a && gone_b)) {
                 // ---- scores: sc[qt][block]: keys s_key[0] (rows 2 t, 2 t + 1), s_key[1] ------------------------
@@ -364,26 +367,24 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 #pragma unroll
                     for (int k = 0; k < 8; ++k) sc[qt][k >> 2][k & 3] = 0.f;
 #pragma unroll
-                for (int j = 0; j < D / 32; ++j)
+                for (int j = 0; j < D / 32; ++j) {
+                    uint2 q[kTiles][2];
+#pragma unroll
+                    for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) q[qt][e] = lds_u32x2(q_at + (uint32_t)((qt * (D / 16) + 2 * j + e) * 256));
 #pragma unroll
                     for (int blk = 0; blk < 2; ++blk) {
                         uint32_t u[4];                                   // parts 2 j (rows g, g + 8), 2 j + 1
-                        ldmatrix4(u, ktile + ((k_at + blk * 16 * D) ^ (uint32_t)(32 * j)));
+                        ldmatrix4(u, base + ((k_at + blk * 16 * D) ^ (uint32_t)(32 * j)));
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const uint32_t k16[4] = {widen_lo(u[2 * e]), widen_lo(u[2 * e + 1]), widen_hi(u[2 * e]), widen_hi(u[2 * e + 1])};
 #pragma unroll
-                            for (int qt = 0; qt < kTiles; ++qt) mma_f16(sc[qt][blk], k16, qb[qt][2 * j + e][0], qb[qt][2 * j + e][1]);
+                            for (int qt = 0; qt < kTiles; ++qt) mma_f16(sc[qt][blk], k16, q[qt][e].x, q[qt][e].y);
                         }
                     }
-                // ---- s in base 2, mask -------------------------------------------------------------------------
-#pragma unroll
-                for (int qt = 0; qt < kTiles; ++qt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float fa = cq[qt][e] * sa.x, fb = cq[qt][e] * sb.x;
-                        sc[qt][0][e] *= fa; sc[qt][0][2 + e] *= fa; sc[qt][1][e] *= fb; sc[qt][1][2 + e] *= fb;
-                    }
+                }
                 const bool part = !all || gone_a || gone_b;
                 uint32_t keep[2] = {0xffffffffu, 0xffffffffu};           // bytes of V whose keys some query sees
                 if (part) {
@@ -400,25 +401,27 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         keep[blk] = 0u;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const int j = c0 + 32 * half + 16 * blk + key_of(4 * t + k);
+                            const int j = c0 + 16 * blk + key_of(4 * t + k);
                             if (!gone && j < len && (j > max(q_first, 0) - p.window || j < p.sinks)) keep[blk] |= 0xffu << (8 * k);
                         }
                     }
                 }
-                // ---- running reference ---------------------------------------------------------------------------
-                float mx[kTiles][2];
+                // ---- running reference; scores in base 2 are sc * f (f above 0, so that a hidden one stays -infinity) --
+                float mx[kTiles][2], f[kTiles][2][2];
                 bool rises = false;
 #pragma unroll
                 for (int qt = 0; qt < kTiles; ++qt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        mx[qt][e] = fmaxf(max3(sc[qt][0][e], sc[qt][0][2 + e], sc[qt][1][e]), sc[qt][1][2 + e]);
+                        f[qt][e][0] = fmaxf(cq[qt][e] * sa.x, 1.17549435e-38f);
+                        f[qt][e][1] = fmaxf(cq[qt][e] * sb.x, 1.17549435e-38f);
+                        mx[qt][e] = fmaxf(fmaxf(sc[qt][0][e], sc[qt][0][2 + e]) * f[qt][e][0], fmaxf(sc[qt][1][e], sc[qt][1][2 + e]) * f[qt][e][1]);
                         rises |= mx[qt][e] > m[qt][e] + 14.f;
                     }
                 if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
                     for (int qt = 0; qt < kTiles; ++qt) {
-                        float f[2];
+                        float back[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             float top = mx[qt][e];
@@ -426,18 +429,18 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                             const float m_new = fmaxf(m[qt][e], top - 6.f);
-                            f[e] = m[qt][e] == -INFINITY ? 1.f : ex2_approx(m[qt][e] - m_new);
+                            back[e] = m[qt][e] == -INFINITY ? 1.f : ex2_approx(m[qt][e] - m_new);
                             m[qt][e] = m_new;
-                            l[qt][e] *= f[e];
+                            l[qt][e] *= back[e];
                         }
-                        times(qt, f[0], f[1]);
+                        times(qt, back[0], back[1]);
                     }
                 }
                 // ---- the unit of O~ ----------------------------------------------------------------------------
                 const float va = gone_a ? sb.y : sa.y, vb = gone_b ? sa.y : sb.y;
                 const float v_most = fmaxf(va, vb), v_least = fminf(va, vb);
                 if (!(v_most <= unit && v_least * 64.f >= unit)) {
-                    if (unit == 0.f) unit = v_most;
+                    if (unit == 0.f) { unit = v_most; inv_unit = pow2_inverse(unit); }
                     else if (v_most > unit * 5.421010862427522e-20f) to_unit(v_most);        // 2^-64; below, it does not count
                 }
                 // ---- weights ---------------------------------------------------------------------------------------
@@ -449,7 +452,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             float &x = sc[qt][k >> 1][2 * (k & 1) + e];
-                            x = ex2_approx(x - mu);
+                            x = ex2_approx(fmaf(x, f[qt][e][k >> 1], -mu));
                             l[qt][e] += x;
                         }
                     }
@@ -457,12 +460,12 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                 const bool apart = v_least * 64.f < unit && va != vb;
 #pragma unroll 1
                 for (int pass = 0; pass < (apart ? 2 : 1); ++pass) {
-                    float fa = va / unit, fb = vb / unit;                // powers of two up to 1
+                    float fa = va * inv_unit, fb = vb * inv_unit;        // powers of two up to 1
                     if (apart) {
                         const float mine = pass ? vb : va;
                         if (mine > unit * 5.421010862427522e-20f && mine != unit) to_unit(mine);
-                        fa = pass ? 0.f : mine / unit;
-                        fb = pass ? mine / unit : 0.f;
+                        fa = pass ? 0.f : mine * inv_unit;
+                        fb = pass ? mine * inv_unit : 0.f;
                     }
                     uint32_t pb[kTiles][2][2];                           // per block: places 0 .. 7, 8 .. 15 of row g
 #pragma unroll
@@ -475,7 +478,7 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) {
                         uint32_t u[4];                                   // per block: elements 16 c + g, 16 c + 8 + g
-                        ldmatrix_bytes(u, vtile + (v_at ^ (uint32_t)(16 * c)));
+                        ldmatrix_bytes(u, base + (v_at ^ (uint32_t)(16 * c)));
                         if (part) { u[0] &= keep[0]; u[1] &= keep[0]; u[2] &= keep[1]; u[3] &= keep[1]; }
 #pragma unroll
                         for (int blk = 0; blk < 2; ++blk) {
@@ -486,8 +489,9 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     }
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(empty(s));
+            __syncwarp();                                                // every lane has read the slot
+            copy_step();
+            slot = slot + 1 < L::kSlots ? slot + 1 : 0;
         }
 
         // ---- join the warps that share these rows ----------------------------------------------------------
@@ -507,113 +511,140 @@ kv_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             for (int k = 0; k < D / 8; ++k)                              // element 8 k + g of rows 2 t, 2 t + 1
                 join[((warp * kTiles + qt) * (D / 8) + k) * 32 + lane] =
                     make_float2(o[qt][k >> 1][2 * (k & 1)] * unit, o[qt][k >> 1][2 * (k & 1) + 1] * unit);
-        named_bar_sync(1, L::kWarps * 32);
+        __syncthreads();
         const bool whole = tiles == a.n;
-        constexpr int kSame = 2 * kTileGroups;                           // warps with the same rows: group, group + kGroups, ...
-        if (*s_abort == 0)
-            for (int x = (warp / kGroups) * 32 + lane; x < 8 * kTiles * (D / 4); x += kSame * 32) {
-                const int rr = x / (D / 4), d0 = x % (D / 4) * 4, r = row_base + rr;
-                if (r >= p.R) continue;
-                float M = -INFINITY, Lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int x = tid; x < 8 * kTiles * (D / 4); x += L::kThreads) {
+            const int rr = x / (D / 4), d0 = x % (D / 4) * 4, r = row_base + rr;
+            if (r >= p.R) continue;
+            float M = -INFINITY, Lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int y = 0; y < kSame; ++y) M = fmaxf(M, ml[(group + y * kGroups) * 8 * kTiles + rr].x);
-                const float Mu = M == -INFINITY ? 0.f : M;
+            for (int y = 0; y < L::kWarps; ++y) M = fmaxf(M, ml[y * 8 * kTiles + rr].x);
+            const float Mu = M == -INFINITY ? 0.f : M;
 #pragma unroll
-                for (int y = 0; y < kSame; ++y) {
-                    const int from = group + y * kGroups;
-                    const float2 own = ml[from * 8 * kTiles + rr];
-                    const float f = ex2_approx(own.x - Mu);
-                    Lsum += f * own.y;
-                    const float *src = reinterpret_cast<const float *>(join + ((from * kTiles + (rr >> 3)) * (D / 8) + (d0 >> 3)) * 32) +
-                                       ((d0 & 7) * 4 + (rr & 7) / 2) * 2 + (rr & 1);
+            for (int y = 0; y < L::kWarps; ++y) {
+                const float2 own = ml[y * 8 * kTiles + rr];
+                const float f = ex2_approx(own.x - Mu);
+                Lsum += f * own.y;
+                const float *src = reinterpret_cast<const float *>(join + ((y * kTiles + (rr >> 3)) * (D / 8) + (d0 >> 3)) * 32) +
+                                   ((d0 & 7) * 4 + (rr & 7) / 2) * 2 + (rr & 1);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[k] += f * src[8 * k];
-                }
-                if (whole) {
-                    kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
-                } else {
-                    const int64_t row = (int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + group * 8 * kTiles + rr;
-                    *reinterpret_cast<float4 *>(p.part_o + row * D + d0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                    if (d0 == 0) p.part_ml[row] = make_float2(M, Lsum);
-                }
+                for (int k = 0; k < 4; ++k) acc[k] += f * src[8 * k];
             }
+            if (whole) {
+                kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
+            } else {
+                const int64_t row = (int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + rr;
+                *reinterpret_cast<float4 *>(p.part_o + row * D + d0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                if (d0 == 0) p.part_ml[row] = make_float2(M, Lsum);
+            }
+        }
         if (tid == 0 && a.i == 0 && !whole) p.desc[blockIdx.x] = make_int2(a.b * heads + a.hr, (w + a.n - 1) / per);
-        named_bar_sync(1, L::kWarps * 32);                               // before the buffers are written again
+        __syncthreads();                                                 // before the buffers, and q, are written again
         w += tiles;
     }
 }
 
-// Joins the parts of the item that begins in CTA blockIdx.x of the kernel above and ends in a later one, in the CTAs' order.
-// Blocks (CTA, rows): 512 / D rows, four elements per thread.
+// Joins the parts of the item that begins in CTA blockIdx.x of the kernel above and ends in a later one, in the order of
+// the CTAs.  Blocks (CTA, row); D / 4 threads per part, four elements each, 512 / D parts at a time.  The loads of the parts' O~ do
+// not wait for their maxima, so that a block takes three round trips to memory, whatever the number of parts up to 4 x 512 / D.
 template <typename T16, int D, int kRows>
 __global__ void __launch_bounds__(128)
 kv_join_kernel(const KvAttnParams p)
 {
+    constexpr int kLanes = D / 4, kSide = 128 / kLanes, kEach = 4;
+    __shared__ float s_m[4];
+    __shared__ float s_o[kSide][kLanes][5];
     allow_next_kernel();
     await_previous_kernel();
     const int2 what = p.desc[blockIdx.x];
     if (what.x < 0) return;
-    const int heads = p.Hkv * p.groups, hr = what.x % heads;
-    const int rr = blockIdx.y * (512 / D) + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
+    const int heads = p.Hkv * p.groups, hr = what.x % heads, rr = blockIdx.y;
     const int r = hr % p.groups * kRows + rr;
     if (r >= p.R) return;
     const int parts = what.y - (int)blockIdx.x + 1;
+    const int x = threadIdx.x % kLanes, side = threadIdx.x / kLanes;
     auto row = [&](int k) { return (int64_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * kRows + rr; };
-    float m = -INFINITY, l = 0.f;
-    for (int k = 0; k < parts; ++k) m = fmaxf(m, p.part_ml[row(k)].x);
+    float4 u[kEach];
+    float2 ml[kEach];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int k = k0 + i * kSide + side;
+            u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            ml[i] = make_float2(-INFINITY, 0.f);
+            if (k < parts) {
+                u[i] = *reinterpret_cast<const float4 *>(p.part_o + row(k) * D + 4 * x);
+                ml[i] = p.part_ml[row(k)];
+            }
+        }
+    };
+    load(0);
+    float m = -INFINITY;
+    for (int k = threadIdx.x; k < parts; k += 128) m = fmaxf(m, p.part_ml[row(k)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) s_m[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
     const float mu = m == -INFINITY ? 0.f : m;
-    float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-        const float2 ml = p.part_ml[row(k)];
-        const float4 u = *reinterpret_cast<const float4 *>(p.part_o + row(k) * D + d0);
-        const float f = ex2_approx(ml.x - mu);
-        l += f * ml.y;
-        o[0] += f * u.x; o[1] += f * u.y; o[2] += f * u.z; o[3] += f * u.w;
+    float acc[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < parts; k0 += kEach * kSide) {
+        if (k0 > 0) load(k0);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const float f = ex2_approx(ml[i].x - mu);
+            acc[0] += f * u[i].x; acc[1] += f * u[i].y; acc[2] += f * u[i].z; acc[3] += f * u[i].w;
+            acc[4] += f * ml[i].y;
+        }
     }
-    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, d0, o, m, l);
+#pragma unroll
+    for (int e = 0; e < 5; ++e) s_o[side][x][e] = acc[e];
+    __syncthreads();
+    if (side > 0) return;
+#pragma unroll
+    for (int e = 0; e < 5; ++e)
+#pragma unroll
+        for (int k = 1; k < kSide; ++k) acc[e] += s_o[k][x][e];
+    const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
+    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, 4 * x, o, m, acc[4]);
 }
 
-// Rows of a kv head go to a CTA 8, 16, 32 or 64 at a time, so that its K and V are read once wherever that can be.  A warp serves
-// 8 or 16 of them, so up to 16 a tile is widened once; 32 rows take two groups of warps, 64 four (one CTA per SM).
-struct KvShape { int rows, groups, ctas; };
-static inline KvShape kv_shape(int R)
+// Rows of a kv head go to a CTA 8 or 16 (D = 64: up to 32) at a time, as many as its registers hold; more are items of their own,
+// which CTAs work on at about the same time, so that most of what they read again comes from L2.
+struct KvShape { int tiles, groups, ctas; };
+static inline KvShape kv_shape(int R, int D)
 {
     KvShape s;
-    s.rows = R <= 8 ? 8 : R <= 16 ? 16 : R <= 32 ? 32 : 64;
-    s.groups = (R + s.rows - 1) / s.rows;
-    s.ctas = num_sms() * (s.rows < 64 ? 2 : 1);
+    s.tiles = R <= 8 ? 1 : R <= 16 || D == 128 ? 2 : 4;
+    s.groups = (R + 8 * s.tiles - 1) / (8 * s.tiles);
+    s.ctas = num_sms() * (D == 64 && s.tiles < 4 ? 3 : 2);
     return s;
 }
 // Bytes: part_o, part_ml, desc
 static inline size_t kv_workspace(const KvShape &s, int D)
 {
-    const size_t rows = (size_t)s.ctas * 2 * s.rows;
+    const size_t rows = (size_t)s.ctas * 2 * 8 * s.tiles;
     return rows * D * 4 + rows * 8 + (size_t)s.ctas * 8;
 }
 
-template <typename T16, int D, int kTiles, int kGroups, int kTileGroups>
-static inline baps_status kv_attention_launch(const CUtensorMap &mk, const CUtensorMap &mv, const KvAttnParams &p, int ctas,
-                                              cudaStream_t stream)
+template <typename T16, int D, int kTiles>
+static inline baps_status kv_attention_launch(const KvAttnParams &p, int ctas, cudaStream_t stream)
 {
-    using L = KvLayout<D, kTiles, kGroups, kTileGroups>;
-    if (cudaFuncSetAttribute(kv_attention_kernel<T16, D, kTiles, kGroups, kTileGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    using L = KvLayout<D, kTiles>;
+    if (cudaFuncSetAttribute(kv_attention_kernel<T16, D, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              L::dyn_bytes(kKvMaxB)) != cudaSuccess)
         return BAPS_ERR_CUDA;
-    const baps_status s = launch_kernel(kv_attention_kernel<T16, D, kTiles, kGroups, kTileGroups>, (unsigned)ctas, L::kThreads,
-                                        (size_t)L::dyn_bytes(p.B), stream, mk, mv, p);
+    const baps_status s = launch_kernel(kv_attention_kernel<T16, D, kTiles>, (unsigned)ctas, L::kThreads, (size_t)L::dyn_bytes(p.B), stream, p);
     if (s != BAPS_OK) return s;
-    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)ctas, (unsigned)((L::kRows * D + 511) / 512)), 128, 0, stream, p);
+    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)ctas, (unsigned)(p.R < L::kRows ? p.R : L::kRows)), 128, 0, stream, p);
 }
 
-template <typename T16, int D>
-static inline baps_status kv_attention_rows(const CUtensorMap &mk, const CUtensorMap &mv, const KvAttnParams &p,
-                                            const KvShape &s, cudaStream_t stream)
+template <typename T16>
+static inline baps_status kv_attention_shape(const KvAttnParams &p, int D, const KvShape &s, cudaStream_t stream)
 {
-    if (s.rows == 8) return kv_attention_launch<T16, D, 1, 1, 2>(mk, mv, p, s.ctas, stream);
-    if (s.rows == 16) return kv_attention_launch<T16, D, 2, 1, 2>(mk, mv, p, s.ctas, stream);
-    if (s.rows == 32) return kv_attention_launch<T16, D, 2, 2, 1>(mk, mv, p, s.ctas, stream);
-    return kv_attention_launch<T16, D, 2, 4, 1>(mk, mv, p, s.ctas, stream);
+    if (D == 128) return s.tiles == 1 ? kv_attention_launch<T16, 128, 1>(p, s.ctas, stream) : kv_attention_launch<T16, 128, 2>(p, s.ctas, stream);
+    if (s.tiles == 4) return kv_attention_launch<T16, 64, 4>(p, s.ctas, stream);
+    return s.tiles == 1 ? kv_attention_launch<T16, 64, 1>(p, s.ctas, stream) : kv_attention_launch<T16, 64, 2>(p, s.ctas, stream);
 }
 
 } // namespace baps

@@ -32,7 +32,7 @@ baps_status check_cache(const baps_kv_cache *c)
     if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return BAPS_ERR_INVALID_ARG;
     if (c->n_pages <= 0 || c->Hkv <= 0) return BAPS_ERR_INVALID_ARG;
     if ((c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) || (c->D != 64 && c->D != 128)) return BAPS_ERR_UNSUPPORTED;
-    if ((int64_t)c->n_pages * c->Hkv * c->page > 0x7fffffffLL || c->Hkv > 32767) return BAPS_ERR_UNSUPPORTED;   // 32-bit TMA row coordinate
+    if ((int64_t)c->n_pages * c->Hkv * c->page > 0x7fffffffLL || c->Hkv > 32767) return BAPS_ERR_UNSUPPORTED;   // 32-bit row number
     if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return BAPS_ERR_ALIGNMENT;
     return BAPS_OK;
 }
@@ -122,7 +122,7 @@ size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D)
 {
     if (B <= 0 || B > kKvMaxB || H <= 0 || Hkv <= 0 || H % Hkv != 0 || T <= 0 || T > 16 || (D != 64 && D != 128)) return 0;
     if ((int64_t)T * (H / Hkv) > 0x7fffffff - 64) return 0;
-    return kv_workspace(kv_shape(T * (H / Hkv)), D);
+    return kv_workspace(kv_shape(T * (H / Hkv), D), D);
 }
 
 baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_kv_cache *cache, const int32_t *table,
@@ -147,32 +147,26 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
         for (int i = 0; i < 6; ++i) s[i] = strides[i];
     }
     if (!have_device()) return BAPS_ERR_CUDA;
-    const KvShape shape = kv_shape(T * (H / cache->Hkv));
+    const KvShape shape = kv_shape(T * (H / cache->Hkv), D);
     if (workspace_bytes < kv_workspace(shape, D)) return BAPS_ERR_INVALID_ARG;
     // tiles of the whole call, at most: a 32-bit count
     int64_t tiles = (places + kKvTile - 1) / kKvTile;
     const int64_t seen = ((int64_t)window + T) / kKvTile + sinks / kKvTile + 4;
     tiles = tiles < seen ? tiles : seen;
     if (tiles * B * cache->Hkv * shape.groups > 0x7fffffffLL - 4096) return BAPS_ERR_UNSUPPORTED;
-    const uint64_t rows = (uint64_t)cache->n_pages * cache->Hkv * cache->page;
-    const uint32_t box = cache->page < kKvTile ? cache->page : kKvTile;
-    CUtensorMap mk, mv;
-    if (!make_tmap_codes(&mk, cache->k, rows, D, box) || !make_tmap_codes(&mv, cache->v, rows, D, box)) return BAPS_ERR_CUDA;
     KvAttnParams p;
     p.q = q; p.out = out; p.lse = lse;
     p.qs_b = s[0]; p.qs_h = s[1]; p.qs_t = s[2]; p.os_b = s[3]; p.os_h = s[4]; p.os_t = s[5];
-    p.table = table; p.lengths = lengths; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
+    p.table = table; p.lengths = lengths; p.k = cache->k; p.v = cache->v; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
     p.width = table_width; p.B = B; p.H = H; p.Hkv = cache->Hkv; p.T = T; p.G = H / cache->Hkv; p.R = T * p.G; p.groups = shape.groups;
     p.n_pages = cache->n_pages; p.page = cache->page; p.window = window; p.sinks = sinks;
     p.c = base2_scale(scale, D);
-    const size_t part_rows = (size_t)shape.ctas * 2 * shape.rows;
+    const size_t part_rows = (size_t)shape.ctas * 2 * 8 * shape.tiles;
     p.part_o = static_cast<float *>(workspace);
     p.part_ml = reinterpret_cast<float2 *>(p.part_o + part_rows * D);
     p.desc = reinterpret_cast<int2 *>(p.part_ml + part_rows);
     cudaStream_t cs = as_stream(stream);
-    if (dtype == BAPS_DTYPE_F16)
-        return D == 128 ? kv_attention_rows<__half, 128>(mk, mv, p, shape, cs) : kv_attention_rows<__half, 64>(mk, mv, p, shape, cs);
-    return D == 128 ? kv_attention_rows<__nv_bfloat16, 128>(mk, mv, p, shape, cs) : kv_attention_rows<__nv_bfloat16, 64>(mk, mv, p, shape, cs);
+    return dtype == BAPS_DTYPE_F16 ? kv_attention_shape<__half>(p, D, shape, cs) : kv_attention_shape<__nv_bfloat16>(p, D, shape, cs);
 }
 
 size_t baps_kv_pages_workspace(int rows, int n_pages)

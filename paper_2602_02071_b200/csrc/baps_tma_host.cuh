@@ -58,20 +58,6 @@ static inline bool make_tmap_heads16(CUtensorMap *map, const void *base, bool ha
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Map of 8-bit elements [rows, D], D = 64 or 128 = one swizzle row, read in boxes of box_rows x D.
-static inline bool make_tmap_codes(CUtensorMap *map, const void *base, uint64_t rows, int D, uint32_t box_rows)
-{
-    EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)D, rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)D};
-    const cuuint32_t box[2] = {(cuuint32_t)D, box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Map of a row-major matrix of 8-bit elements [rows, cols] (cols contiguous, cols * 1 byte = one
 // 128-byte swizzle row) read in boxes of box_rows x 128 columns with the 128-byte swizzle.
 static inline bool make_tmap_u8_rows(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols,
