@@ -7,20 +7,6 @@
 
 namespace baps {
 
-// Whether the compiled kernel has the registers that its roles share out (see split_fits); asked once per kernel, the
-// answer is part of the module image.
-template <auto kernel>
-static inline bool has_registers_for(const RegisterSplit &split)
-{
-    static std::atomic<bool> yes{false};
-    if (yes.load(std::memory_order_relaxed)) return true;
-    cudaFuncAttributes a;
-    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) { (void)cudaGetLastError(); return false; }
-    if (!split_fits(split, a.numRegs)) return false;
-    yes.store(true, std::memory_order_relaxed);
-    return true;
-}
-
 struct AttnLaunch { CUtensorMap mq, mk, mv; AttnTcParams p; long long nblocks; cudaStream_t stream; };
 template <auto kernel, int kSmem>
 static inline baps_status launch_attention(const AttnLaunch &a, const RegisterSplit &split = kTcSplit)

@@ -10,18 +10,24 @@
 // One CTA owns two consecutive 128-row query tiles (t = 0, 1) of one head, which share the K / V stream: the tiles that
 // hold first tokens, then those from the window's left edge to the diagonal.  A stream takes part in the key tiles that
 // some row of its own sees.
-//   warps 0-3, 4-7  softmax of stream 0, 1: a thread per row
-//   warp 8          TMA producer: Q tiles, then K_0, V_0, K_1, ... through a ring of 128 x D tiles
-//   warp 9          MMA issuer, per key tile and stream: P V, then Q K^T of the stream's next key tile into the same columns
-//   warps 10, 11    zero what stands behind a sequence's end in its last V tile (a weight of 0 does not hide a NaN)
-// TMEM (512 columns): S_0 | S_1 | O_0 | O_1, 128 columns each; the 16-bit weights of column
-// quarter q overwrite columns [32 q, 32 q + 16) of S_t.
+//   warps 0-15      softmax: stream t = w / 8; two threads per row, 64 key columns each, in two chunks of 32
+//   warp 16         TMA producer: Q tiles, then K_0, V_0, K_1, ... through a ring of 128 x D tiles
+//   warp 17         MMA issuer, per key tile and stream: P V for the keys of the second chunks as soon as their weights are
+//                   there, then for the others, and Q K^T of the stream's next key tile into the same columns
+//   warps 18, 19    zero what stands behind a sequence's end in its last V tile (a weight of 0 does not hide a NaN)
+// TMEM (512 columns): S_0 | S_1 | O_0 | O_1, 128 columns each; the 16-bit weights of column quarter q overwrite columns
+// [32 q, 32 q + 16) of S_t.
 // Tensor memory is taken after the kernel ahead has ended and before the next one may start.  All waits are bounded; after an
 // expired one every later wait returns at once and the roles run on to the common teardown without storing.
+//
+// What bounds it: the chain of a stream, scores to weights to products, as in paired_attention_tc_kernel.  One thread per row, four
+// warps per stream: 3900 cycles for a pair of key tiles, in which the exponentials need 2048 of their pipe and the products 1024 of the
+// tensor core, and 0 to 100 % of the exponentials on the FMA pipe made no difference.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include "baps_common.cuh"
+#include "baps_register_split.cuh"
 #include "baps_sm100.cuh"
 #include "baps_tma_host.cuh"
 
@@ -32,20 +38,23 @@ struct WindowParams {
     float *lse;
     const int32_t *lengths;
     int64_t os_b, os_h, os_s;      // strides of out, elements
-    int B, H, Hkv, S, window, sinks, npairs;
+    int B, H, Hkv, S, window, sinks, nitems;          // nitems: work items per head, of one or two query tiles
     float c;
 };
 
-constexpr int kWinThreads = 384;
-
-template <int D>
+template <int D, int kStreams>
 struct WinLayout {
-    static constexpr int kTileBytes = 128 * D * 2, kStages = D == 128 ? 4 : 8;
+    static constexpr RegisterSplit kSplit = kStreams == 2 ? kTcSplit : kWindowSplit;
+    static constexpr int kSoftmaxWarps = kSplit.many_threads / 32;
+    static constexpr int kCtasPerSm = D == 64 && kStreams == 1 ? 2 : 1;
+    static constexpr int kTileBytes = 128 * D * 2, kStages = D == 128 || kStreams == 1 ? 4 : 8;
     static constexpr int kQOff = 0;
-    static constexpr int kKvOff = 2 * kTileBytes;
+    static constexpr int kKvOff = kStreams * kTileBytes;
     static constexpr int kBarOff = kKvOff + kStages * kTileBytes;
-    // q_full, s_full[2], p_full[2], o_done[2], v_there, v_clean, kv_full[stages], kv_empty[stages]
-    static constexpr int kMiscOff = (kBarOff + (9 + 2 * kStages) * 8 + 15) & ~15;
+    static constexpr int kTmemCols = 256 * kStreams;                   // S, then O, 128 columns each per stream
+    // q_full, s_full[2], p_full[2][2], o_done[2], v_there, v_clean, kv_full[stages], kv_empty[stages]
+    static constexpr int kXchgOff = (kBarOff + (11 + 2 * kStages) * 8 + 15) & ~15;     // float xchg[2 tiles][128][2]
+    static constexpr int kMiscOff = kXchgOff + 2 * 128 * 2 * 4;
     static constexpr int kDynBytes = kMiscOff + 16 + 1024;
 };
 
@@ -87,19 +96,20 @@ __device__ __forceinline__ float max8w(const uint32_t *x)
                 fmaxf(__uint_as_float(x[6]), __uint_as_float(x[7])));
 }
 
-template <typename T16, int D>
-__global__ void __launch_bounds__(kWinThreads, 1)
+template <typename T16, int D, int kStreams>
+__global__ void __launch_bounds__(WinLayout<D, kStreams>::kSplit.threads, WinLayout<D, kStreams>::kCtasPerSm)
 window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                         const __grid_constant__ CUtensorMap mv, const WindowParams p)
 {
     using namespace sm100;
-    using L = WinLayout<D>;
+    using L = WinLayout<D, kStreams>;
+    constexpr int kProducer = L::kSoftmaxWarps, kIssuer = kProducer + 1, kOCol = 128 * kStreams;
     constexpr bool kHalf = __is_same(T16, __half);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sbase = smem_u32(smem);
     auto bar = [&](int i) { return sbase + L::kBarOff + 8u * (uint32_t)i; };
-    constexpr int BQ = 0, BS = 1, BP = 3, BD = 5, BV = 7, BC = 8, BKF = 9, BKE = 9 + L::kStages;
+    constexpr int BQ = 0, BS = 1, BP = 3, BD = 7, BV = 9, BC = 10, BKF = 11, BKE = 11 + L::kStages;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + L::kMiscOff);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + L::kMiscOff + 4);
 
@@ -107,15 +117,15 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     // blocks: query heads of a kv head next to each other, later rows (more keys, while the window fills) first
     const int heads = p.B * p.H;
     const int h = (int)(blockIdx.x % (unsigned)heads) % p.H, b = (int)(blockIdx.x % (unsigned)heads) / p.H;
-    const int q0 = 2 * (p.npairs - 1 - (int)(blockIdx.x / (unsigned)heads));
+    const int q0 = kStreams * (p.nitems - 1 - (int)(blockIdx.x / (unsigned)heads));
     const int hk = h / (p.H / p.Hkv);
 
     await_previous_kernel();
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.S) : p.S;
     if (q0 * 128 >= len) return;
     // last rows of the two query tiles; the second is absent where the sequence ends in the first
-    const bool two = (q0 + 1) * 128 < len;
-    const int last0 = min(q0 * 128 + 127, len - 1), last1 = min(q0 * 128 + 255, len - 1);
+    const bool two = kStreams == 2 && (q0 + 1) * 128 < len;
+    const int last0 = min(q0 * 128 + 127, len - 1), last1 = min(q0 * 128 + 128 * kStreams - 1, len - 1);
     const KeyTiles kt = key_tiles(q0 * 128, last1, p.window, p.sinks, 7);
     const KeyTiles mine0 = key_tiles(q0 * 128, last0, p.window, p.sinks, 7);
     const KeyTiles mine1 = key_tiles(min(q0 * 128 + 128, last1), last1, p.window, p.sinks, 7);
@@ -128,21 +138,24 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
 
     if (tid == 0) {
         mbar_init(bar(BQ), 1);
-        for (int t = 0; t < 2; ++t) { mbar_init(bar(BS + t), 1); mbar_init(bar(BP + t), 4); mbar_init(bar(BD + t), 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(bar(BS + t), 1); mbar_init(bar(BD + t), 1); }
+        for (int i = 0; i < 4; ++i) mbar_init(bar(BP + i), 8);
         mbar_init(bar(BV), 1);
         mbar_init(bar(BC), 2);
         for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(BKF + s), 1); mbar_init(bar(BKE + s), 1); }
         mbar_fence_init();
         *s_abort = 0;
     }
-    if (warp == 9) { tmem_alloc(smem_u32(s_tmem), 512); tmem_relinquish(); }
+    if (warp == kIssuer) { tmem_alloc(smem_u32(s_tmem), L::kTmemCols); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     allow_next_kernel();
     const uint32_t tmem = *s_tmem;
 
-    if (warp == 8) {
+    if (warp >= L::kSoftmaxWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kSplit.few));
+        if (warp == kProducer) {
         // ======================= TMA producer ======================================================
         if (lane == 0) {
             mbar_arrive_expect_tx(bar(BQ), (two ? 2u : 1u) * L::kTileBytes);
@@ -167,7 +180,7 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
                 }
             }
         }
-    } else if (warp == 9) {
+        } else if (warp == kIssuer) {
         // ======================= MMA issuer ========================================================
         constexpr uint32_t fmt = kHalf ? 0u : (1u << 7) | (1u << 10);
         constexpr uint32_t idesc_qk = (make_idesc_bf16(128, 128, false) & ~((7u << 7) | (7u << 10))) | fmt;
@@ -186,16 +199,19 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             }
             mma_commit(bar(BS + t));
         };
-        auto mma_pv = [&](int t, int j, bool more) {
+        // O_t += P V_j over the keys of one half of the weights: 32-column quarters 1 and 3 (first), then 0 and 2
+        auto mma_pv = [&](int t, int j, int half, bool more) {
             const uint32_t vd = sdesc_lo(sbase + L::kKvOff + stage_of(2 * j + 1) * L::kTileBytes, 16384);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                mma_ts_lo(tmem + 256 + t * 128, tmem + t * 128 + (ks >> 1) * 32 + (ks & 1) * 8, vd + ks * 128, idesc_pv, more || ks > 0);
+            for (int i = 0; i < 4; ++i) {
+                const int quarter = (i >> 1) * 2 + 1 - half, ks = 2 * quarter + (i & 1);
+                mma_ts_lo(tmem + kOCol + t * 128, tmem + t * 128 + quarter * 32 + (i & 1) * 8, vd + ks * 128, idesc_pv, half || i || more);
+            }
         };
         // A stream's next Q K^T is issued behind its P V, into the same columns.
         int done[2] = {0, 0};                          // key tiles that the stream has been through
         auto next_of = [&](int t, int j) { while (j < J && !takes(t, j)) ++j; return j; };
-        int nj[2] = {next_of(0, 0), next_of(1, 0)};    // the tile whose scores were asked for last (J: no more)
+        int nj[2] = {next_of(0, 0), kStreams == 2 ? next_of(1, 0) : J};    // the tile whose scores were asked for last (J: no more)
         int k_there = 0, k_freed = 0;                  // K tiles waited for, and given back
         bool ok = wait_all(bar(BQ), 0, 0x410);
         auto need_k = [&](int j) {
@@ -205,7 +221,7 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
         auto free_k = [&] {
             for (; k_freed < J && k_freed <= min(nj[0], nj[1]); ++k_freed) mma_commit(bar(BKE + stage_of(2 * k_freed)));
         };
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kStreams; ++t)
             if (nj[t] < J) {
                 need_k(nj[t]);
                 if (!ok) break;
@@ -222,16 +238,21 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
                 __syncwarp();
                 ok = wait_all(bar(BC), 0, 0x421);
             }
-            for (int t = 0; ok && t < 2; ++t) {
+            for (int t = 0; ok && t < kStreams; ++t) {
                 if (nj[t] != j) continue;
                 const int nx = next_of(t, j + 1);
                 if (nx < J) need_k(nx);
-                ok = ok && wait_all(bar(BP + t), (uint32_t)(done[t] & 1), 0x430 + t);
+                ok = ok && wait_all(bar(BP + 2 * t), (uint32_t)(done[t] & 1), 0x430 + t);
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (leader) mma_pv(t, j, 0, done[t] > 0);
+                __syncwarp();
+                ok = wait_all(bar(BP + 2 * t + 1), (uint32_t)(done[t] & 1), 0x432 + t);
                 if (!ok) break;
                 tc_fence_after_sync();
                 nj[t] = nx;
                 if (leader) {
-                    mma_pv(t, j, done[t] > 0);
+                    mma_pv(t, j, 1, true);
                     if (nx < J) mma_qk(t, nx);
                     else mma_commit(bar(BD + t));
                     free_k();
@@ -243,13 +264,13 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             if (ok && leader) mma_commit(bar(BKE + stage_of(2 * j + 1)));
             __syncwarp();
         }
-    } else if (warp >= 10) {
+        } else {
         // ======================= rows behind the sequence's end ====================================
         if (ragged) {
             const int l = 2 * J - 1, first = len & 127;
             if (__all_sync(0xffffffffu, mbar_wait(bar(BV), 0, s_abort, &g_async_status, 0x440))) {
                 const uint32_t stage = sbase + L::kKvOff + stage_of(l) * L::kTileBytes;
-                for (int i = (warp - 10) * 32 + lane; i < (128 - first) * (D / 8); i += 64) {
+                for (int i = (warp - kIssuer - 1) * 32 + lane; i < (128 - first) * (D / 8); i += 64) {
                     const int row = first + i / (D / 8), part = i % (D / 8);
                     sts_u32x4(stage + (uint32_t)((part >> 3) * 16384 + row * 128 + (part & 7) * 16), make_uint4(0, 0, 0, 0));
                 }
@@ -258,13 +279,18 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
                 if (lane == 0) mbar_arrive(bar(BC));
             }
         }
-    } else if (warp < (two ? 8 : 4)) {
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kSplit.many));
         // ======================= softmax warps =====================================================
-        const int t = warp >> 2, q4 = warp & 3;
+        const int t = warp >> 3, q4 = warp & 3, ch = (warp >> 2) & 1;
+        if (t == 0 || two) {
         const int row = q4 * 32 + lane;                               // of the query tile
         const int r = (q0 + t) * 128 + row;                           // of the sequence
         const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
-        const uint32_t s_addr = tmem + lane_sel + t * 128, o_addr = tmem + lane_sel + 256 + t * 128;
+        const uint32_t s_addr = tmem + lane_sel + t * 128 + ch * 64, o_addr = tmem + lane_sel + kOCol + t * 128 + ch * (D / 2);
+        const uint32_t xrow = sbase + L::kXchgOff + (uint32_t)((t * 128 + row) * 8);
+        const uint32_t row_bar = 1 + t * 4 + q4;                      // the two warps that share these rows
         const int r_first = (q0 + t) * 128, r_last = r_first + 127;
         const float c = p.c;
         const uint64_t c2 = pack2(c, c);
@@ -277,39 +303,41 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             const bool all = c0 + 127 <= r_first && (c0 > r_last - p.window || c0 + 127 < p.sinks);
             mbar_wait(bar(BS + t), (uint32_t)(n & 1), s_abort, &g_async_status, 0x450 + t);
             tc_fence_after_sync();
-            // columns c0 + 32 i .. + 31 that the row sees, as bits
-            auto visible = [&](int i) -> uint32_t {
-                const int b0 = c0 + 32 * i;
-                auto below = [&](int x) -> uint32_t { x -= b0; return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; };
-                const uint32_t near = below(r + 1) & ~below(r - p.window + 1);
-                return near | (below(p.sinks) & below(r + 1));
-            };
-            auto load = [&](int i, uint32_t (&x)[32]) { tmem_ld32(s_addr + 32 * i, x); };
-            auto mask = [&](int i, uint32_t (&x)[32]) {
-                if (!all) {
-                    const uint32_t see = visible(i);
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = (see >> k & 1u) ? x[k] : 0xFF800000u;
-                }
-            };
-            auto max32 = [&](const uint32_t (&x)[32]) {
-                return max3(max3(max8w(&x[0]), max8w(&x[8]), max8w(&x[16])), max8w(&x[24]), -INFINITY);
-            };
             uint32_t x[32], y[32];
-            load(0, x); load(1, y);
+            tmem_ld32(s_addr, x);
+            tmem_ld32(s_addr + 32, y);
             tmem_wait_ld();
-            mask(0, x); mask(1, y);
-            float mx = fmaxf(max32(x), max32(y));
-            load(2, x); load(3, y);
-            tmem_wait_ld();
-            mask(2, x); mask(3, y);
-            mx = max3(mx, max32(x), max32(y)) * c;
-            if (__any_sync(0xffffffffu, mx > m + 8.f)) {
-                const float m_new = fmaxf(m, mx);
+            bool no_x = false, no_y = false;              // no row of the warp sees any key of the chunk
+            if (!all) {
+                // columns b0 .. b0 + 31 that the row sees, as bits
+                auto visible = [&](int b0) -> uint32_t {
+                    auto below = [&](int v) -> uint32_t { v -= b0; return v <= 0 ? 0u : v >= 32 ? 0xffffffffu : (1u << v) - 1u; };
+                    return (below(r + 1) & ~below(r - p.window + 1)) | (below(p.sinks) & below(r + 1));
+                };
+                const uint32_t sx = visible(c0 + ch * 64), sy = visible(c0 + ch * 64 + 32);
+                no_x = !__any_sync(0xffffffffu, sx != 0u);
+                no_y = !__any_sync(0xffffffffu, sy != 0u);
+                if (!no_x && !__all_sync(0xffffffffu, sx == 0xffffffffu)) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) x[k] = (sx >> k & 1u) ? x[k] : 0xFF800000u;
+                }
+                if (!no_y && !__all_sync(0xffffffffu, sy == 0xffffffffu)) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) y[k] = (sy >> k & 1u) ? y[k] : 0xFF800000u;
+                }
+            }
+            auto max32 = [&](const uint32_t (&v)[32]) { return fmaxf(max3(max8w(&v[0]), max8w(&v[8]), max8w(&v[16])), max8w(&v[24])); };
+            const float mx = fmaxf(no_x ? -INFINITY : max32(x), no_y ? -INFINITY : max32(y)) * c;
+            // ---- the maximum moves in some of these rows: both threads of a row go on with the same one -------
+            if (named_bar_or(row_bar, 64, mx > m + 8.f)) {
+                sts_f32(xrow + 4u * (uint32_t)ch, mx);
+                named_bar_sync(row_bar, 64);
+                const float2 both = lds_f32x2(xrow);
+                const float m_new = max3(m, both.x, both.y);
                 const float f = m == -INFINITY ? 1.f : ex2_approx(m - m_new);      // (nothing there yet: l = 0, O~ = 0)
                 if (n > 0) {
 #pragma unroll 1
-                    for (int i0 = 0; i0 < D; i0 += 16) {
+                    for (int i0 = 0; i0 < D / 2; i0 += 16) {
                         uint32_t o[16];
                         tmem_ld16(o_addr + i0, o);
                         tmem_wait_ld();
@@ -324,13 +352,17 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             const float mu = m == -INFINITY ? 0.f : -m;
             const uint64_t m2 = pack2(mu, mu);
             uint64_t s01 = 0ull, s23 = 0ull;
-            auto weights = [&](int i, const uint32_t (&x)[32]) {
+            auto weights = [&](int i, const uint32_t (&v)[32], bool none) {
                 uint32_t pk[16];
+                if (none) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) pk[k] = 0u;
+                } else
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) {
                     float w[4];
-                    unpack2(fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), w[0], w[1]);
-                    unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), c2, m2), w[2], w[3]);
+                    unpack2(fma2(pack2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), c2, m2), w[0], w[1]);
+                    unpack2(fma2(pack2(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), c2, m2), w[2], w[3]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = ex2_approx(w[e]);
                     s01 = add2(s01, pack2(w[0], w[1]));
@@ -340,17 +372,16 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
                 }
                 tmem_st16(s_addr + 32 * i, pk);
             };
-            weights(2, x);
-            weights(3, y);
-            load(0, x); load(1, y);
-            tmem_wait_ld();
-            mask(0, x); mask(1, y);
-            weights(0, x);
-            weights(1, y);
-            tmem_wait_st();
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(BP + t));
+            auto arrive = [&](int half) {
+                tmem_wait_st();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BP + 2 * t + half));
+            };
+            weights(1, y, no_y);
+            arrive(0);                                    // the tensor core starts on the keys of the second chunks
+            weights(0, x, no_x);
+            arrive(1);
             float a0, a1, a2, a3;
             unpack2(s01, a0, a1); unpack2(s23, a2, a3);
             l += (a0 + a1) + (a2 + a3);
@@ -359,11 +390,16 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
         // ---- O = O~ / l, through the (now idle) Q tile so that the stores are whole rows --------------------
         const bool good = mbar_wait(bar(BD + t), 0, s_abort, &g_async_status, 0x460 + t) && *s_abort == 0;
         tc_fence_after_sync();
+        named_bar_sync(row_bar, 64);                      // the partner has read the last maxima
+        sts_f32(xrow + 4u * (uint32_t)ch, l);
+        named_bar_sync(row_bar, 64);
+        const float2 both = lds_f32x2(xrow);
+        l = both.x + both.y;
         const float inv = 1.f / l;
         constexpr int kChunks = D / 8;                               // 16-byte parts of a row
         const uint32_t stage = sbase + L::kQOff + t * L::kTileBytes;
 #pragma unroll 1
-        for (int i0 = 0; i0 < D; i0 += 16) {
+        for (int i0 = 0; i0 < D / 2; i0 += 16) {
             uint32_t rr[16];
             tmem_ld16(o_addr + i0, rr);
             tmem_wait_ld();
@@ -371,39 +407,53 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = pack16<T16>(__uint_as_float(rr[2 * i]) * inv, __uint_as_float(rr[2 * i + 1]) * inv);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                sts_u32x4(stage + (uint32_t)(row * 2 * D + (((i0 >> 3) + i) ^ (row & (kChunks - 1))) * 16),
+            for (int i = 0; i < 2; ++i) {
+                const int part = (ch * (D / 2) + i0) / 8 + i;
+                sts_u32x4(stage + (uint32_t)(row * 2 * D + (part ^ (row & (kChunks - 1))) * 16),
                           make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            }
         }
-        __syncwarp();
+        named_bar_sync(row_bar, 64);
         T16 *out = reinterpret_cast<T16 *>(p.out) + b * p.os_b + h * p.os_h;
         constexpr int kRowsAtOnce = 32 / kChunks;
 #pragma unroll 4
-        for (int i = 0; i < kChunks; ++i) {
-            const int rw = q4 * 32 + i * kRowsAtOnce + lane / kChunks, part = lane % kChunks;
+        for (int i = 0; i < kChunks / 2; ++i) {
+            const int rw = q4 * 32 + ch * 16 + i * kRowsAtOnce + lane / kChunks, part = lane % kChunks;
             const uint4 v = lds_u32x4(stage + (uint32_t)(rw * 2 * D + (part ^ (rw & (kChunks - 1))) * 16));
             const int64_t gr = (int64_t)(q0 + t) * 128 + rw;
             if (good && gr < len) *reinterpret_cast<uint4 *>(out + gr * p.os_s + part * 8) = v;
         }
-        if (good && p.lse && r < len) p.lse[((int64_t)b * p.H + h) * p.S + r] = (m + log2f(l)) * 0.69314718055994531f;
+        if (good && ch == 0 && p.lse && r < len) p.lse[((int64_t)b * p.H + h) * p.S + r] = (m + log2f(l)) * 0.69314718055994531f;
+        }
     }
 
     // ---- teardown -------------------------------------------------------------------------------
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 9) { __syncwarp(); tmem_dealloc(tmem, 512); }
+    if (warp == kIssuer) { __syncwarp(); tmem_dealloc(tmem, L::kTmemCols); }
 }
 
-template <typename T16, int D>
-static inline baps_status window_launch(const CUtensorMap *maps, const WindowParams &p, cudaStream_t stream)
+template <typename T16, int D, int kStreams>
+static inline baps_status window_launch(const CUtensorMap *maps, WindowParams &p, cudaStream_t stream)
 {
-    const long long blocks = (long long)p.B * p.H * p.npairs;
+    using L = WinLayout<D, kStreams>;
+    p.nitems = (p.S + 128 * kStreams - 1) / (128 * kStreams);
+    const long long blocks = (long long)p.B * p.H * p.nitems;
     if (blocks > 0x7fffffffLL) return BAPS_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(window_attention_kernel<T16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             WinLayout<D>::kDynBytes) != cudaSuccess)
+    if (!has_registers_for<window_attention_kernel<T16, D, kStreams>>(L::kSplit) ||
+        cudaFuncSetAttribute(window_attention_kernel<T16, D, kStreams>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
         return BAPS_ERR_CUDA;
-    return launch_kernel(window_attention_kernel<T16, D>, (unsigned)blocks, kWinThreads, (size_t)WinLayout<D>::kDynBytes, stream,
+    return launch_kernel(window_attention_kernel<T16, D, kStreams>, (unsigned)blocks, L::kSplit.threads, (size_t)L::kDynBytes, stream,
                          maps[0], maps[1], maps[2], p);
+}
+
+// One or two query tiles per CTA.
+template <typename T16>
+static inline baps_status window_shape(const CUtensorMap *maps, WindowParams &p, int D, cudaStream_t stream)
+{
+    const bool small = (long long)p.B * p.H * ((p.S + 255) / 256) < num_sms();
+    if (D == 64) return window_launch<T16, 64, 1>(maps, p, stream);
+    return small ? window_launch<T16, 128, 1>(maps, p, stream) : window_launch<T16, 128, 2>(maps, p, stream);
 }
 
 } // namespace baps

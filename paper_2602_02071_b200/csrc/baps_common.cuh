@@ -6,6 +6,7 @@
 #include <mutex>
 #include <cuda_runtime.h>
 #include "../../include/baps.h"
+#include "baps_register_split.cuh"
 
 namespace baps {
 
@@ -73,6 +74,20 @@ inline baps_status launch_kernel(void (*kernel)(P...), dim3 grid, int threads, s
         return BAPS_ERR_CUDA;
     }
     return launch_status();
+}
+
+// Whether the compiled kernel has the registers that its roles share out (see split_fits); asked once per kernel, the
+// answer is part of the module image.
+template <auto kernel>
+static inline bool has_registers_for(const RegisterSplit &split)
+{
+    static std::atomic<bool> yes{false};
+    if (yes.load(std::memory_order_relaxed)) return true;
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) { (void)cudaGetLastError(); return false; }
+    if (!split_fits(split, a.numRegs)) return false;
+    yes.store(true, std::memory_order_relaxed);
+    return true;
 }
 
 inline bool have_device()

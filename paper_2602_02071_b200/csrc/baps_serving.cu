@@ -80,10 +80,8 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
     p.out = out; p.lse = lse; p.lengths = lengths;
     p.os_b = s[9]; p.os_h = s[10]; p.os_s = s[11];
     p.B = B; p.H = H; p.Hkv = Hkv; p.S = S; p.window = window; p.sinks = sinks;
-    p.npairs = (S + 255) / 256;
     p.c = base2_scale(scale, D);
-    if (half) return D == 128 ? window_launch<__half, 128>(maps, p, as_stream(stream)) : window_launch<__half, 64>(maps, p, as_stream(stream));
-    return D == 128 ? window_launch<__nv_bfloat16, 128>(maps, p, as_stream(stream)) : window_launch<__nv_bfloat16, 64>(maps, p, as_stream(stream));
+    return half ? window_shape<__half>(maps, p, D, as_stream(stream)) : window_shape<__nv_bfloat16>(maps, p, D, as_stream(stream));
 }
 
 baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const void *v_new, const int64_t *strides,
