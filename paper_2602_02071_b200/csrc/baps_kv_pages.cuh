@@ -218,7 +218,11 @@ kv_compact_count_kernel(const KvCompactParams p)
 
 // Every block: used pages before its chunk and in all, then the ranks of its pages.  A used page at or behind n_live is
 // mover number (used pages before it) - (used pages before n_live), a free page before n_live is hole number (free pages
-// before it); both lists are as long as each other.
+// before it); both lists are as long as each other.  kCounted: the chunks' counts are there; otherwise every block
+// reads all counts of references (up to kCompactDirect pages, 256 KB from L2), which saves a launch.
+// page_map of a mover is for the time being -2 - its number counted from the end.
+constexpr int kCompactDirect = 65536;
+template <bool kCounted>
 __global__ void __launch_bounds__(1024)
 kv_compact_lists_kernel(const KvCompactParams p)
 {
@@ -227,10 +231,19 @@ kv_compact_lists_kernel(const KvCompactParams p)
     await_previous_kernel();
     const int chunk = blockIdx.x;
     int before = 0, live = 0, sum;
-    for (int k = threadIdx.x; k < p.chunks; k += 1024) {
-        const int n = p.chunk_live[k];
-        live += n;
-        if (k < chunk) before += n;
+    if constexpr (kCounted) {
+        for (int k = threadIdx.x; k < p.chunks; k += 1024) {
+            const int n = p.chunk_live[k];
+            live += n;
+            if (k < chunk) before += n;
+        }
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < p.pool.n_pages; i += 1024) {
+            const int used = p.refs[i] > 0 ? 1 : 0;
+            live += used;
+            if (i < chunk * 1024) before += used;
+        }
     }
     block_scan(live, s_warp, sum);
     live = sum;
@@ -240,14 +253,13 @@ kv_compact_lists_kernel(const KvCompactParams p)
     const int refs = i < p.pool.n_pages ? p.refs[i] : 0;
     const int rank = before + block_scan(refs > 0 ? 1 : 0, s_warp, sum);       // used pages before page i
     if (i < p.pool.n_pages) {
-        // holes before n_live = used pages behind it: the mover of rank `rank` (0 .. live - 1) is number live - 1 - rank
-        // from the end
-        if (refs > 0 && i >= live) p.movers[live - 1 - rank] = i;
+        const bool mover = refs > 0 && i >= live;
+        if (mover) p.movers[live - 1 - rank] = i;
         if (refs <= 0 && i < live) p.holes[i - rank] = i;
-        p.page_map[i] = refs > 0 && i < live ? i : -1;
+        p.page_map[i] = mover ? -2 - (live - 1 - rank) : refs > 0 ? i : -1;
         p.new_refs[i] = refs > 0 && i < live ? refs : 0;
     }
-    // the hole that is last: all free pages before n_live
+    // movers = used pages behind the first n_live
     if (i == live - 1) *p.n_moves = live - rank - (refs > 0 ? 1 : 0);
     if (chunk == 0 && threadIdx.x == 0) {
         *p.n_live = live;
@@ -255,32 +267,33 @@ kv_compact_lists_kernel(const KvCompactParams p)
     }
 }
 
-// Blocks (move, part), striding over the moves.
+// The first table_blocks blocks rewrite the table (an entry that a block of movers has not settled yet gives the same), the
+// others copy, (move, part), striding over the moves.
 __global__ void __launch_bounds__(256)
-kv_compact_move_kernel(const KvCompactParams p)
+kv_compact_move_kernel(const KvCompactParams p, int table_blocks, int parts)
 {
     allow_next_kernel();
     await_previous_kernel();
     const int n = *p.n_moves;
-    for (int k = blockIdx.x; k < n; k += gridDim.x) {
+    if ((int)blockIdx.x < table_blocks) {
+        const int64_t entries = (int64_t)p.rows * p.width;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (int64_t)table_blocks * 256) {
+            const int e = p.table[i];
+            int to = e >= 0 && e < p.pool.n_pages ? *const_cast<volatile int32_t *>(p.page_map + e) : -1;
+            if (to < -1) to = p.holes[n - 1 - (-2 - to)];
+            p.new_table[i] = to;
+        }
+        return;
+    }
+    const int first = ((int)blockIdx.x - table_blocks) / parts, part = ((int)blockIdx.x - table_blocks) % parts;
+    const int step = ((int)gridDim.x - table_blocks) / parts;
+    for (int k = first; k < n; k += step) {
         const int src = p.movers[n - 1 - k], dst = p.holes[k];
-        copy_page(p.pool, src, dst, blockIdx.y, gridDim.y);
-        if (blockIdx.y == 0 && threadIdx.x == 0) {
+        copy_page(p.pool, src, dst, part, parts);
+        if (part == 0 && threadIdx.x == 0) {
             p.page_map[src] = dst;
             p.new_refs[dst] = p.refs[src];
         }
-    }
-}
-
-__global__ void __launch_bounds__(256)
-kv_compact_table_kernel(const KvCompactParams p)
-{
-    allow_next_kernel();
-    await_previous_kernel();
-    const int64_t n = (int64_t)p.rows * p.width;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int e = p.table[i];
-        p.new_table[i] = e >= 0 && e < p.pool.n_pages ? p.page_map[e] : -1;
     }
 }
 
@@ -297,15 +310,18 @@ static inline baps_status kv_fork_launch(const KvForkParams &p, cudaStream_t str
 
 static inline baps_status kv_compact_launch(const KvCompactParams &p, cudaStream_t stream)
 {
-    baps_status s = launch_kernel(kv_compact_count_kernel, (unsigned)p.chunks, 1024, 0, stream, p);
-    if (s == BAPS_OK) s = launch_kernel(kv_compact_lists_kernel, (unsigned)p.chunks, 1024, 0, stream, p);
-    const int64_t per = copy_parts(p.pool.page_bytes), want = 16LL * num_sms() / per;
-    const unsigned blocks = (unsigned)(want < p.pool.n_pages ? (want > 0 ? want : 1) : p.pool.n_pages);
-    if (s == BAPS_OK) s = launch_kernel(kv_compact_move_kernel, dim3(blocks, (unsigned)per), 256, 0, stream, p);
-    const int64_t entries = (int64_t)p.rows * p.width;
-    if (s != BAPS_OK || entries == 0) return s;
-    const int64_t tb = (entries + 255) / 256;
-    return launch_kernel(kv_compact_table_kernel, (unsigned)(tb < 2048 ? tb : 2048), 256, 0, stream, p);
+    baps_status s = BAPS_OK;
+    if (p.pool.n_pages <= kCompactDirect) {
+        s = launch_kernel(kv_compact_lists_kernel<false>, (unsigned)p.chunks, 1024, 0, stream, p);
+    } else {
+        s = launch_kernel(kv_compact_count_kernel, (unsigned)p.chunks, 1024, 0, stream, p);
+        if (s == BAPS_OK) s = launch_kernel(kv_compact_lists_kernel<true>, (unsigned)p.chunks, 1024, 0, stream, p);
+    }
+    if (s != BAPS_OK) return s;
+    const int64_t parts = copy_parts(p.pool.page_bytes), want = 16LL * num_sms() / parts;
+    const int64_t moves = want < p.pool.n_pages ? (want > 0 ? want : 1) : p.pool.n_pages;
+    const int64_t wide = ((int64_t)p.rows * p.width + 255) / 256, table_blocks = wide < 512 ? wide : 512;
+    return launch_kernel(kv_compact_move_kernel, (unsigned)(table_blocks + moves * parts), 256, 0, stream, p, (int)table_blocks, (int)parts);
 }
 
 } // namespace baps

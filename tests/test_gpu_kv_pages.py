@@ -118,6 +118,14 @@ def test_compact_large_pages_and_ends():
     check_compact(pool(70, 3, 128, 64, 1), [], [0, 1] * 35)
 
 
+def test_compact_of_a_pool_too_large_to_be_read_by_every_block():
+    n_pages = 70001
+    g = torch.Generator().manual_seed(3)
+    refs = (torch.rand(n_pages, generator=g) < 0.4).int()
+    table = torch.randint(-1, n_pages, (50, 40), generator=g).tolist()
+    check_compact(pool(n_pages, 1, 16, 64, 1), table, refs.tolist())
+
+
 def test_fork_and_compact_in_a_graph():
     page, n_pages, rows = 16, 60, 4
     table, lengths, refs = batch(rows, 4, page, n_pages, 5, most=48)
