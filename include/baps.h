@@ -271,8 +271,8 @@ baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const 
  * A row that sees no key (a position below 0, pages that are not there) gives zeros and an lse of -infinity.
  * Only pages that hold a visible key are read.  lse: NULL or device float [B, H, T].  strides: NULL for contiguous, else
  * 6 int64 in elements, multiples of 8: batch, head and token of q, then of out.
- * workspace: device memory, 16-byte aligned, at least baps_kv_attention_workspace() bytes, contents irrelevant before and
- * after; calls that may run at the same time need one each.
+ * workspace: device memory, 16-byte aligned, at least baps_kv_attention_workspace() bytes (NULL if those are 0), contents
+ * irrelevant before and after; calls that may run at the same time need one each.
  * Value scales of a sequence and head that are more than 2^64 apart: the smaller values may count as zero.
  * Results are the same from call to call.  dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q and out).  scale: 0: 1/sqrt(D).
  * Supported: T <= 16; H % Hkv == 0; B <= 4096.                                                             */
@@ -280,8 +280,9 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
                               int table_width, const int32_t *lengths, const int64_t *strides, int B, int H, int T,
                               int window, int sinks, float scale, int dtype, void *workspace, size_t workspace_bytes,
                               baps_stream stream);
-/* Bytes of workspace for these sizes on the current device; 0 for sizes that baps_kv_attention refuses. */
-size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D);
+/* Bytes of workspace for these sizes on the current device; 0 where none is needed (workspace may be NULL then: short contexts,
+ * by table_width and window) and for sizes that baps_kv_attention refuses. */
+size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page, int table_width, int window, int sinks);
 
 /* ---- Pages: rows of a batch rebuilt from parents --------------------------------------------------------
  * One step of a serving loop's bookkeeping, without the host knowing a length: new row i of the table becomes a

@@ -88,7 +88,7 @@ def load() -> ctypes.CDLL:
     lib.baps_kv_compact.argtypes = [vp, vp, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
     for n in EXPORTS[:16]:
         getattr(lib, n).restype = i
-    lib.baps_kv_attention_workspace.argtypes = [i, i, i, i, i]
+    lib.baps_kv_attention_workspace.argtypes = [i] * 9
     lib.baps_kv_attention_workspace.restype = sz
     lib.baps_kv_pages_workspace.argtypes = [i, i]
     lib.baps_kv_pages_workspace.restype = sz
@@ -470,14 +470,15 @@ def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_
         _check("baps_kv_append", status)
 
 
-@functools.lru_cache(maxsize=256)
-def _attention_workspace(device: int, B: int, H: int, Hkv: int, T: int, D: int) -> int:
-    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D))
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(device: int, *sizes: int) -> int:
+    return int(load().baps_kv_attention_workspace(*sizes))
 
 
-def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int) -> int:
-    """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: sizes that it refuses)."""
-    return _attention_workspace(_device(), B, H, Hkv, T, D)
+def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int, page: int, table_width: int, window: Optional[int] = None,
+                           sinks: int = 0) -> int:
+    """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: none, or sizes that it refuses)."""
+    return _attention_workspace(_device(), B, H, Hkv, T, D, page, table_width, _window(window), int(sinks))
 
 
 def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int] = None, sinks: int = 0, scale: float = 0.0,
@@ -491,8 +492,9 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     device = cache.here()
     shape = q.shape
     B, H, T, D = shape
-    _, Hkv, _, Dc = cache.k.shape
+    _, Hkv, page, Dc = cache.k.shape
     rows, width = table.shape
+    window, sinks = _window(window), int(sinks)
     if D != Dc or rows != B:
         raise ValueError("q does not match the cache, or table is not [B,width]")
     if out is None:
@@ -505,17 +507,17 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     else:
         lse_ptr = None
     if workspace is None:
-        n = _attention_workspace(_device(), B, H, Hkv, T, D) or 16
-        workspace = cache.k.new_empty((n,))
+        n = _attention_workspace(_device(), B, H, Hkv, T, D, page, width, window, sinks)
+        ws_ptr = (workspace := cache.k.new_empty((n,))).data_ptr() if n else None
     elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor on q's device")
     else:
-        n = workspace.numel()
+        n, ws_ptr = workspace.numel(), workspace.data_ptr()
     st = _pack("6q", *_stride3(q, q, shape, "q"), *_stride3(out, q, shape, "out"))
     status = load().baps_kv_attention(
         q.data_ptr(), out.data_ptr(), lse_ptr, cache.struct, _buffer(table, torch.int32, device, (B, width), "table"), width,
-        _buffer(lengths, torch.int32, device, (B,), "lengths"), st, B, H, T, _window(window), int(sinks), float(scale), code,
-        workspace.data_ptr(), n, _stream())
+        _buffer(lengths, torch.int32, device, (B,), "lengths"), st, B, H, T, window, sinks, float(scale), code, ws_ptr, n,
+        _stream())
     if status:
         _check("baps_kv_attention", status)
     return (out, lse) if want_lse else out

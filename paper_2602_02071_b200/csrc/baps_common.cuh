@@ -60,20 +60,28 @@ __device__ __forceinline__ T *await_previous_kernel(T *p)
     return p;
 }
 
+// cluster: CTAs per cluster, along x; 0: what the kernel itself says, if anything.
 template <typename... P, typename... A>
-inline baps_status launch_kernel(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A... args)
+inline baps_status launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, int threads, size_t smem, cudaStream_t stream, A... args)
 {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
+    cfg.attrs = attr; cfg.numAttrs = cluster ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
         (void)cudaGetLastError();
         return BAPS_ERR_CUDA;
     }
     return launch_status();
+}
+template <typename... P, typename... A>
+inline baps_status launch_kernel(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A... args)
+{
+    return launch_clusters(kernel, grid, 0, threads, smem, stream, args...);
 }
 
 // Whether the compiled kernel has the registers that its roles share out (see split_fits); asked once per kernel, the

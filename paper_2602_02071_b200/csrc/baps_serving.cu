@@ -116,11 +116,12 @@ baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const 
     return cache->D == 128 ? kv_append_page<__nv_bfloat16, 128>(p, cache->page, s) : kv_append_page<__nv_bfloat16, 64>(p, cache->page, s);
 }
 
-size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D)
+size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page, int table_width, int window, int sinks)
 {
     if (B <= 0 || B > kKvMaxB || H <= 0 || Hkv <= 0 || H % Hkv != 0 || T <= 0 || T > 16 || (D != 64 && D != 128)) return 0;
-    if ((int64_t)T * (H / Hkv) > 0x7fffffff - 64) return 0;
-    return kv_workspace(kv_shape(T * (H / Hkv), D), D);
+    if ((page != 16 && page != 32 && page != 64 && page != 128) || table_width <= 0 || window < 1 || sinks < 0) return 0;
+    if ((int64_t)T * (H / Hkv) > 65536) return 0;
+    return kv_workspace(kv_shape(T * (H / Hkv), D, (int64_t)B * Hkv, kv_most_tiles(page, table_width, T, window, sinks)), D);
 }
 
 baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_kv_cache *cache, const int32_t *table,
@@ -130,7 +131,7 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
 {
     baps_status st = check_cache(cache);
     if (st != BAPS_OK) return st;
-    if (!q || !out || !table || !lengths || !workspace) return BAPS_ERR_INVALID_ARG;
+    if (!q || !out || !table || !lengths) return BAPS_ERR_INVALID_ARG;
     if (B <= 0 || H <= 0 || T <= 0 || table_width <= 0 || H % cache->Hkv != 0) return BAPS_ERR_INVALID_ARG;
     st = check_softmax(window, sinks, scale, dtype);
     if (st != BAPS_OK) return st;
@@ -144,14 +145,13 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
         if (!strides_ok(strides, 6)) return BAPS_ERR_INVALID_ARG;
         for (int i = 0; i < 6; ++i) s[i] = strides[i];
     }
-    if (!have_device()) return BAPS_ERR_CUDA;
-    const KvShape shape = kv_shape(T * (H / cache->Hkv), D);
-    if (workspace_bytes < kv_workspace(shape, D)) return BAPS_ERR_INVALID_ARG;
-    // tiles of the whole call, at most: a 32-bit count
-    int64_t tiles = (places + kKvTile - 1) / kKvTile;
-    const int64_t seen = ((int64_t)window + T) / kKvTile + sinks / kKvTile + 4;
-    tiles = tiles < seen ? tiles : seen;
+    const int64_t tiles = kv_most_tiles(cache->page, table_width, T, window, sinks);
+    const KvShape shape = kv_shape(T * (H / cache->Hkv), D, (int64_t)B * cache->Hkv, tiles);
+    const size_t need = kv_workspace(shape, D);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return BAPS_ERR_INVALID_ARG;
+    // tiles of the whole call are a 32-bit count
     if (tiles * B * cache->Hkv * shape.groups > 0x7fffffffLL - 4096) return BAPS_ERR_UNSUPPORTED;
+    if (!have_device()) return BAPS_ERR_CUDA;
     KvAttnParams p;
     p.q = q; p.out = out; p.lse = lse;
     p.qs_b = s[0]; p.qs_h = s[1]; p.qs_t = s[2]; p.os_b = s[3]; p.os_h = s[4]; p.os_t = s[5];

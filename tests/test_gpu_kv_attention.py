@@ -20,8 +20,9 @@ pytestmark = pytest.mark.gpu
 def make(B, H, Hkv, T, D, page, lengths, dtype, seed=0, spare=3, width=None, window=serving.NONE, sinks=0):
     """Inputs on the CPU and GPU; pages in random order, those that no query sees given back (-1)."""
     g = torch.Generator().manual_seed(seed)
-    width = width or max(1, max(-(-n // page) for n in lengths))
-    n_pages = B * width + spare
+    most = max(1, max(-(-n // page) for n in lengths))
+    width = width or most
+    n_pages = B * most + spare
     table = torch.full((B, width), -1, dtype=torch.int32)
     order = torch.randperm(n_pages, generator=g).to(torch.int32)
     at = 0
@@ -60,32 +61,37 @@ def check(q, state, table, lengths, window, sinks, scale=0.0, got=None):
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 @pytest.mark.parametrize("H,Hkv,T,D", [(1, 1, 1, 64), (8, 2, 1, 128), (16, 1, 1, 128), (6, 2, 5, 64), (24, 1, 1, 128), (8, 1, 8, 128),
                                        (8, 1, 8, 64), (12, 2, 16, 128)])
-def test_heads_and_pages(dtype, page, H, Hkv, T, D):
-    q, *rest = make(3, H, Hkv, T, D, page, [200, 17, 64], dtype)
+@pytest.mark.parametrize("room", [0, 9000])                          # a wide table takes the call to the even cut
+def test_heads_and_pages(dtype, page, H, Hkv, T, D, room):
+    q, *rest = make(3, H, Hkv, T, D, page, [200, 17, 64], dtype, width=room // page, spare=3)
+    assert (binding.kv_attention_workspace(3, H, Hkv, T, D, page, rest[1].shape[1]) > 0) == (room > 0)
     check(q, *rest, serving.NONE, 0)
 
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("T", [1, 3])
 @pytest.mark.parametrize("lengths", [[1], [2, 1, 3], [63, 64, 65], [127, 128, 129, 0], [0, 0], [1500], [700, 5, 1100, 64, 0, 333, 1]])
-def test_lengths(D, T, lengths):
-    q, *rest = make(len(lengths), 4, 2, T, D, 32, lengths, torch.bfloat16, seed=T)
+@pytest.mark.parametrize("room", [0, 9000])
+def test_lengths(D, T, lengths, room):
+    q, *rest = make(len(lengths), 4, 2, T, D, 32, lengths, torch.bfloat16, seed=T, width=room // 32)
     check(q, *rest, serving.NONE, 0)
 
 
 @pytest.mark.parametrize("T", [1, 4])
 @pytest.mark.parametrize("page", [16, 64, 128])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (63, 64), (64, 0), (100, 130), (500, 16), (5000, 3), (257, 1000)])
-def test_windows(T, page, window, sinks):
-    q, *rest = make(4, 4, 1, T, 64, page, [900, 300, 70, 3], torch.float16, seed=window, window=window, sinks=sinks)
+@pytest.mark.parametrize("length", [900, 9000])
+def test_windows(T, page, window, sinks, length):
+    q, *rest = make(4, 4, 1, T, 64, page, [length, 300, 70, 3], torch.float16, seed=window, window=window, sinks=sinks)
     check(q, *rest, window, sinks)
 
 
 def test_many_sequences_share_the_ctas_evenly():
     g = torch.Generator().manual_seed(2)
     lengths = torch.randint(0, 400, (300,), generator=g).tolist()
-    q, *rest = make(300, 4, 1, 1, 64, 16, lengths, torch.bfloat16)
-    check(q, *rest, serving.NONE, 0)
+    for width in (25, 100):                                        # a CTA each, and the even cut
+        q, *rest = make(300, 4, 1, 1, 64, 16, lengths, torch.bfloat16, width=width)
+        check(q, *rest, serving.NONE, 0)
 
 
 def test_one_long_sequence_is_split_and_joined():
@@ -227,7 +233,8 @@ def test_refusals():
     assert status(lambda: binding.baps_kv_attention(q, cache, table, n, scale=-1.0)) == -1
     assert status(lambda: binding.baps_kv_attention(q.expand(1, 4, 17, 64).contiguous(), cache, table, n)) == -2
     assert status(lambda: binding.baps_kv_attention(q[:, :3], cache, table, n)) == -1
-    assert status(lambda: binding.baps_kv_attention(q, cache, table, n, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))) == -1
+    wide = torch.full((1, 600), -1, dtype=torch.int32, device="cuda")
+    assert status(lambda: binding.baps_kv_attention(q, cache, wide, n, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))) == -1
     with pytest.raises(ValueError):
         binding.baps_kv_attention(q.float(), cache, table, n)
     with pytest.raises(ValueError):

@@ -79,7 +79,7 @@ def test_append(lib):
 
 
 def test_attention(lib):
-    for bad in (dict(q=None), dict(out=None), dict(table=None), dict(lengths=None), dict(ws=None), dict(B=0), dict(H=3), dict(T=0),
+    for bad in (dict(q=None), dict(out=None), dict(table=None), dict(lengths=None), dict(B=0), dict(H=3), dict(T=0),
                 dict(width=0), dict(window=0), dict(sinks=-1), dict(scale=-0.5), dict(strides=(ctypes.c_int64 * 6)(64, 64, 64, 64, 64, 12))):
         assert attention(lib, **bad) == -1, bad
     for bad in (dict(T=17), dict(B=4097), dict(dtype=binding.DTYPE_F32), dict(width=1 << 28)):
@@ -103,9 +103,14 @@ def test_fork_and_compact(lib):
 
 
 def test_workspaces(lib):
-    size = lib.baps_kv_attention_workspace
-    assert 0 < size(1, 8, 8, 1, 64) < size(1, 8, 8, 1, 128) <= size(1, 64, 8, 2, 128)
-    for refused in ((0, 8, 8, 1, 64), (4097, 8, 8, 1, 64), (1, 8, 3, 1, 64), (1, 8, 8, 17, 64), (1, 8, 8, 1, 96), (1, 8, 8, 0, 64)):
-        assert size(*refused) == 0
+    def size(B=1, H=8, Hkv=8, T=1, D=64, page=16, width=10000, window=1 << 30, sinks=0):
+        return lib.baps_kv_attention_workspace(B, H, Hkv, T, D, page, width, window, sinks)
+
+    assert 0 < size() < size(D=128) <= size(H=64, T=2, D=128)
+    assert size(width=20) == size(window=100) == 0                                     # short contexts need none
+    for refused in (dict(B=0), dict(B=4097), dict(Hkv=3), dict(T=17), dict(D=96), dict(T=0), dict(page=8), dict(width=0), dict(window=0)):
+        assert size(**refused) == 0
+    # a call that needs one is refused without it, or with one that is too small
+    assert attention(lib, width=10000, window=1 << 30, ws=None) == attention(lib, width=10000, window=1 << 30, ws_bytes=1000) == -1
     pages = lib.baps_kv_pages_workspace
     assert pages(0, 1) > 0 and pages(10, 1000) > pages(0, 1000) and pages(-1, 5) == pages(3, 0) == 0
