@@ -61,6 +61,8 @@ struct KvLayout {
     static constexpr int kCtasPerSm = D == 64 && kTiles < 4 ? 3 : 2;
     static constexpr int kSlotBytes = 2 * kKvStep * D;                   // K and V of a step
     static constexpr int kSlots = D == 64 ? (kTiles == 2 ? 3 : 4) : 2;
+    // Three slots and more: the slot that the step before was in is filled while this step's products run, else behind them.
+    static constexpr bool kCopyFirst = kSlots > 2;
     static constexpr int kSlotOff = 0;                                   // [warp][slot]
     static constexpr int kJoinOff = kWarps * kSlots * kSlotBytes;        // [warp][kTiles][D / 8][lane] float2
     static constexpr int kMlOff = kJoinOff + kWarps * kTiles * 8 * D * 4;    // [warp][8 kTiles] (m, l)
@@ -174,15 +176,23 @@ __device__ __forceinline__ KvPlace kv_place(const int *pre, int B, int heads, in
     return a;
 }
 
-// Elements d0 .. d0 + 3 of an output row from O~ and l (against m); d0 = 0 brings the lse along.
+template <typename T16>
+__device__ __forceinline__ T16 from_float(float x)
+{
+    if constexpr (__is_same(T16, __half)) return __float2half_rn(x); else return __float2bfloat16_rn(x);
+}
+__device__ __forceinline__ void kv_store_lse(const KvAttnParams &p, int b, int h, int tq, float m, float l)
+{
+    if (p.lse) p.lse[((int64_t)b * p.H + h) * p.T + tq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+// Elements d0 .. d0 + 3 of an output row from O~ and l (against the maximum m); d0 = 0 brings the lse along.
 template <typename T16>
 __device__ __forceinline__ void kv_store(const KvAttnParams &p, int b, int h, int tq, int d0, const float (&o)[4], float m, float l)
 {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2 *>(reinterpret_cast<T16 *>(p.out) + b * p.os_b + h * p.os_h + tq * p.os_t + d0) =
         make_uint2(pack16<T16>(o[0] * inv, o[1] * inv), pack16<T16>(o[2] * inv, o[3] * inv));
-    if (d0 == 0 && p.lse)
-        p.lse[((int64_t)b * p.H + h) * p.T + tq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    if (d0 == 0) kv_store_lse(p, b, h, tq, m, l);
 }
 
 // kClusters: a cluster of CTAs takes one sequence and head and cuts its tiles evenly; its parts are joined through the CTAs'
@@ -312,7 +322,7 @@ kv_attention_kernel(const KvAttnParams p)
         ++next_k;
         next_slot = next_slot + 1 < L::kSlots ? next_slot + 1 : 0;
     };
-    for (int i = 0; i < L::kSlots; ++i) copy_step();
+    for (int i = 0; i < L::kSlots - (L::kCopyFirst ? 1 : 0); ++i) copy_step();
 
     const int g = lane >> 2, t = lane & 3;
     // What this lane addresses of the first 16 keys of a step (the second 16 and other parts: plus 16 rows, exclusive or, which
@@ -396,8 +406,9 @@ kv_attention_kernel(const KvAttnParams p)
         };
 
         for (; warp + 4 * step < steps_here; ++step) {
-            copies_wait<L::kSlots - 1>();
+            copies_wait<L::kSlots - (L::kCopyFirst ? 2 : 1)>();
             __syncwarp();                                                // what the other lanes copied is there too
+            if constexpr (L::kCopyFirst) copy_step();
             const int u = warp + 4 * step;
             const int c0 = kt.tile(a.i + (w0 + (u >> 1) - w)) * kKvTile + (u & 1) * kKvStep;
             // every query sees every key of the step
@@ -537,7 +548,7 @@ kv_attention_kernel(const KvAttnParams p)
                 }
             }
             __syncwarp();                                                // every lane has read the slot
-            copy_step();
+            if constexpr (!L::kCopyFirst) copy_step();
             slot = slot + 1 < L::kSlots ? slot + 1 : 0;
         }
 
@@ -560,32 +571,58 @@ kv_attention_kernel(const KvAttnParams p)
                     make_float2(o[qt][k >> 1][2 * (k & 1)] * unit, o[qt][k >> 1][2 * (k & 1) + 1] * unit);
         __syncthreads();
         const bool whole = tiles == a.n;
-        for (int x = tid; x < 8 * kTiles * (D / 4); x += L::kThreads) {
-            const int rr = x / (D / 4), d0 = x % (D / 4) * 4, r = row_base + rr;
-            if (r >= p.R) continue;
-            float M = -INFINITY, Lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+        // Each warp joins every fourth of the (rows, 8 elements) entries, a thread what its own lane wrote: element 8 k + g of
+        // rows 2 t, 2 t + 1 (no two lanes in a bank; read by output row, 16 at a time met in one and the join took 3700 cycles)
 #pragma unroll
-            for (int y = 0; y < L::kWarps; ++y) M = fmaxf(M, ml[y * 8 * kTiles + rr].x);
-            const float Mu = M == -INFINITY ? 0.f : M;
+        for (int qt = 0; qt < kTiles; ++qt) {
+            float M[2], Lsum[2], f[2][L::kWarps], inv[2];
+            int64_t to[2];                                               // first element of the row, wherever it goes
 #pragma unroll
-            for (int y = 0; y < L::kWarps; ++y) {
-                const float2 own = ml[y * 8 * kTiles + rr];
-                const float f = ex2_approx(own.x - Mu);
-                Lsum += f * own.y;
-                const float *src = reinterpret_cast<const float *>(join + ((y * kTiles + (rr >> 3)) * (D / 8) + (d0 >> 3)) * 32) +
-                                   ((d0 & 7) * 4 + (rr & 7) / 2) * 2 + (rr & 1);
+            for (int e = 0; e < 2; ++e) {
+                const int rr = 8 * qt + 2 * t + e, r = row_base + rr;
+                M[e] = -INFINITY;
+                Lsum[e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[k] += f * src[8 * k];
+                for (int y = 0; y < L::kWarps; ++y) M[e] = fmaxf(M[e], ml[y * 8 * kTiles + rr].x);
+                const float Mu = M[e] == -INFINITY ? 0.f : M[e];
+#pragma unroll
+                for (int y = 0; y < L::kWarps; ++y) {
+                    const float2 own = ml[y * 8 * kTiles + rr];
+                    f[e][y] = ex2_approx(own.x - Mu);
+                    Lsum[e] += f[e][y] * own.y;
+                }
+                inv[e] = 1.f;
+                if (kClusters) {
+                    to[e] = rr * D;
+                } else if (whole) {
+                    inv[e] = Lsum[e] == 0.f ? 0.f : 1.f / Lsum[e];
+                    to[e] = a.b * p.os_b + (hk * p.G + r / p.T) * p.os_h + r % p.T * p.os_t;
+                } else {
+                    to[e] = ((int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + rr) * D;
+                }
+                if (r >= p.R) to[e] = -1;
+                if (warp == 0 && g == 0 && r < p.R) {
+                    if (kClusters) *reinterpret_cast<float2 *>(smem + L::kRows * D * 4 + rr * 8) = make_float2(M[e], Lsum[e]);
+                    else if (whole) kv_store_lse(p, a.b, hk * p.G + r / p.T, r % p.T, M[e], Lsum[e]);
+                    else p.part_ml[to[e] / D] = make_float2(M[e], Lsum[e]);
+                }
             }
-            if constexpr (kClusters) {                                   // over the slots, which every warp is done with
-                *reinterpret_cast<float4 *>(smem + (rr * D + d0) * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                if (d0 == 0) *reinterpret_cast<float2 *>(smem + L::kRows * D * 4 + rr * 8) = make_float2(M, Lsum);
-            } else if (whole) {
-                kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
-            } else {
-                const int64_t row = (int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + rr;
-                *reinterpret_cast<float4 *>(p.part_o + row * D + d0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                if (d0 == 0) p.part_ml[row] = make_float2(M, Lsum);
+            for (int k = warp; k < D / 8; k += L::kWarps) {
+                float acc[2] = {0.f, 0.f};
+#pragma unroll
+                for (int y = 0; y < L::kWarps; ++y) {
+                    const float2 u = join[((y * kTiles + qt) * (D / 8) + k) * 32 + lane];
+                    acc[0] += f[0][y] * u.x;
+                    acc[1] += f[1][y] * u.y;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (to[e] < 0) continue;
+                    const int64_t at = to[e] + 8 * k + g;
+                    if (kClusters) reinterpret_cast<float *>(smem)[at] = acc[e];     // over the slots, which every warp is done with
+                    else if (whole) reinterpret_cast<T16 *>(p.out)[at] = from_float<T16>(acc[e] * inv[e]);
+                    else p.part_o[at] = acc[e];
+                }
             }
         }
         if constexpr (kClusters) {
