@@ -655,28 +655,35 @@ kv_attention_kernel(const KvAttnParams p)
 }
 
 // Joins the parts of the item that begins in CTA blockIdx.x of the kernel above and ends in a later one, in the order of
-// the CTAs.  Blocks (CTA, row); D / 4 threads per part, four elements each, 512 / D parts at a time.  The loads of the parts' O~ do
-// not wait for their maxima, so that a block takes three round trips to memory, whatever the number of parts up to 4 x 512 / D.
+// the CTAs.  Blocks (CTA, rows); D / 4 threads per row and part, four elements each; 512 / D of those, for as many parts of one
+// row (kRows = 8), or two parts and more rows.  The loads of the parts' O~ do not wait for their maxima, so that a block takes
+// three round trips to memory, whatever the number of parts up to kEach * kSide.
+template <int D, int kRows>
+struct JoinShape {
+    static constexpr int kLanes = D / 4, kSide = kRows == 8 ? 128 / kLanes : 2, kRowsHere = 128 / kLanes / kSide, kEach = 4;
+};
 template <typename T16, int D, int kRows>
 __global__ void __launch_bounds__(128)
 kv_join_kernel(const KvAttnParams p)
 {
-    constexpr int kLanes = D / 4, kSide = 128 / kLanes, kEach = 4;
-    __shared__ float s_m[4];
-    __shared__ float s_o[kSide][kLanes][5];
+    using J = JoinShape<D, kRows>;
+    constexpr int kLanes = J::kLanes, kSide = J::kSide, kEach = J::kEach;
+    __shared__ float s_o[J::kRowsHere][kSide][kLanes][6];
     allow_next_kernel();
     await_previous_kernel();
     const int2 what = p.desc[blockIdx.x];
     if (what.x < 0) return;
-    const int heads = p.Hkv * p.groups, hr = what.x % heads, rr = blockIdx.y;
+    const int x = threadIdx.x % kLanes, side = threadIdx.x / kLanes % kSide, sub = threadIdx.x / (kLanes * kSide);
+    const int heads = p.Hkv * p.groups, hr = what.x % heads, rr = blockIdx.y * J::kRowsHere + sub;
     const int r = hr % p.groups * kRows + rr;
-    if (r >= p.R) return;
+    const bool there = r < p.R;
     const int parts = what.y - (int)blockIdx.x + 1;
-    const int x = threadIdx.x % kLanes, side = threadIdx.x / kLanes;
     auto row = [&](int k) { return (int64_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * kRows + rr; };
-    float4 u[kEach];
-    float2 ml[kEach];
-    auto load = [&](int k0) {
+    // each side its own parts against their own maximum, then the sides together
+    float m = -INFINITY, acc[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; there && k0 < parts; k0 += kEach * kSide) {
+        float4 u[kEach];
+        float2 ml[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int k = k0 + i * kSide + side;
@@ -687,19 +694,13 @@ kv_join_kernel(const KvAttnParams p)
                 ml[i] = p.part_ml[row(k)];
             }
         }
-    };
-    load(0);
-    float m = -INFINITY;
-    for (int k = threadIdx.x; k < parts; k += 128) m = fmaxf(m, p.part_ml[row(k)].x);
+        float top = m;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((threadIdx.x & 31) == 0) s_m[threadIdx.x >> 5] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    const float mu = m == -INFINITY ? 0.f : m;
-    float acc[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < parts; k0 += kEach * kSide) {
-        if (k0 > 0) load(k0);
+        for (int i = 0; i < kEach; ++i) top = fmaxf(top, ml[i].x);
+        const float mu = top == -INFINITY ? 0.f : top, back = ex2_approx(m - mu);
+#pragma unroll
+        for (int e = 0; e < 5; ++e) acc[e] *= back;
+        m = top;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float f = ex2_approx(ml[i].x - mu);
@@ -708,15 +709,24 @@ kv_join_kernel(const KvAttnParams p)
         }
     }
 #pragma unroll
-    for (int e = 0; e < 5; ++e) s_o[side][x][e] = acc[e];
+    for (int e = 0; e < 5; ++e) s_o[sub][side][x][e] = acc[e];
+    s_o[sub][side][x][5] = m;
     __syncthreads();
-    if (side > 0) return;
+    if (side > 0 || !there) return;
+    float all = m;
 #pragma unroll
-    for (int e = 0; e < 5; ++e)
+    for (int k = 1; k < kSide; ++k) all = fmaxf(all, s_o[sub][k][x][5]);
+    const float mu = all == -INFINITY ? 0.f : all, own = ex2_approx(m - mu);
 #pragma unroll
-        for (int k = 1; k < kSide; ++k) acc[e] += s_o[k][x][e];
+    for (int e = 0; e < 5; ++e) acc[e] *= own;
+#pragma unroll
+    for (int k = 1; k < kSide; ++k) {
+        const float f = ex2_approx(s_o[sub][k][x][5] - mu);
+#pragma unroll
+        for (int e = 0; e < 5; ++e) acc[e] += f * s_o[sub][k][x][e];
+    }
     const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
-    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, 4 * x, o, m, acc[4]);
+    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, 4 * x, o, all, acc[4]);
 }
 
 // Rows of a kv head go to a CTA 8 or 16 (D = 64: up to 32) at a time, as many as its registers hold; more are items of their own,
@@ -771,7 +781,8 @@ static inline baps_status kv_attention_launch(const KvAttnParams &p, const KvSha
     const baps_status s = launch_kernel(kv_attention_kernel<T16, D, kTiles, false>, (unsigned)shape.ctas, L::kThreads,
                                         (size_t)L::dyn_bytes(p.B), stream, p);
     if (s != BAPS_OK) return s;
-    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)shape.ctas, (unsigned)(p.R < L::kRows ? p.R : L::kRows)), 128, 0, stream, p);
+    const int rows = p.R < L::kRows ? p.R : L::kRows, at_once = JoinShape<D, L::kRows>::kRowsHere;
+    return launch_kernel(kv_join_kernel<T16, D, L::kRows>, dim3((unsigned)shape.ctas, (unsigned)((rows + at_once - 1) / at_once)), 128, 0, stream, p);
 }
 
 template <typename T16>
