@@ -33,6 +33,11 @@
 
 namespace baps {
 
+#ifdef BAPS_TEST_SKIP_LOAD
+// Test build only: number of the K / V tile load that window_attention_kernel's producer leaves out.  -1: none.
+static __device__ int g_test_skip_window_load = -1;
+#endif
+
 struct WindowParams {
     void *out;
     float *lse;
@@ -166,6 +171,9 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             for (int l = 0; l < 2 * J; ++l) {
                 const int s = stage_of(l);
                 if (!mbar_wait(bar(BKE + s), parity_of(l) ^ 1u, s_abort, &g_async_status, 0x400 + s)) break;
+#ifdef BAPS_TEST_SKIP_LOAD
+                if (l == g_test_skip_window_load) { issued = l + 1; continue; }         // this tile never arrives
+#endif
                 mbar_arrive_expect_tx(bar(BKF + s), L::kTileBytes);
                 for (int hh = 0; hh < D / 64; ++hh)
                     tma_load_4d(sbase + L::kKvOff + s * L::kTileBytes + hh * 16384, (l & 1) ? &mv : &mk, hh * 64,

@@ -52,6 +52,14 @@ baps_status take_serving_status() { return take_async_status(); }
 
 extern "C" {
 
+#ifdef BAPS_TEST_SKIP_LOAD
+// Test build only: as baps_test_skip_kv_load, for the windowed attention.
+int baps_test_skip_window_load(int l)
+{
+    return cudaMemcpyToSymbol(g_test_skip_window_load, &l, sizeof(int)) == cudaSuccess ? 0 : -1;
+}
+#endif
+
 baps_status baps_attention_window_fwd(const void *q, const void *k, const void *v, void *out, float *lse,
                                       const int32_t *lengths, const int64_t *strides, int B, int H, int Hkv, int S,
                                       int D, int window, int sinks, float scale, int dtype, baps_stream stream)
