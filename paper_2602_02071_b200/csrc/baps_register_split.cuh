@@ -18,7 +18,5 @@ constexpr bool split_fits(const RegisterSplit &s, int regs_at_launch)
 // warps; 96 at launch.  attention_d64_kernel: the same with eight; 80 at launch (two CTAs per SM).  All use their pool exactly.
 constexpr RegisterSplit kTcSplit = {640, 64, 512, 104};
 constexpr RegisterSplit kD64Split = {384, 32, 256, 104};
-// window_attention_kernel with one query tile per CTA: 80 at launch (two CTAs per SM); with two it is as attention_tc_kernel.
-constexpr RegisterSplit kWindowSplit = {384, 48, 256, 96};
 
 } // namespace baps

@@ -81,8 +81,9 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
     if (!have_device()) return BAPS_ERR_CUDA;
     CUtensorMap maps[3];
     const bool half = dtype == BAPS_DTYPE_F16;
-    if (!make_tmap_heads16(maps, q, half, B, H, S, D, s) || !make_tmap_heads16(maps + 1, k, half, B, Hkv, S, D, s + 3) ||
-        !make_tmap_heads16(maps + 2, v, half, B, Hkv, S, D, s + 6))
+    const uint32_t keys = (uint32_t)window_box_keys(D);
+    if (!make_tmap_heads16(maps, q, half, B, H, S, D, s, 128) || !make_tmap_heads16(maps + 1, k, half, B, Hkv, S, D, s + 3, keys) ||
+        !make_tmap_heads16(maps + 2, v, half, B, Hkv, S, D, s + 6, keys))
         return BAPS_ERR_CUDA;
     WindowParams p;
     p.out = out; p.lse = lse; p.lengths = lengths;

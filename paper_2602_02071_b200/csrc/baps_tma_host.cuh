@@ -43,15 +43,15 @@ static inline bool make_tmap_bf16_rows(CUtensorMap *map, const void *base, uint6
 }
 
 // Map of 16-bit elements [B, heads, S, D] with any strides (elements, multiples of 8) and contiguous rows, read in boxes of
-// 128 rows x 64 columns with the 128-byte swizzle; rows behind S come as zeros.
+// box_rows rows x 64 columns with the 128-byte swizzle; rows behind S come as zeros.
 static inline bool make_tmap_heads16(CUtensorMap *map, const void *base, bool half, int B, int heads, int S, int D,
-                                     const int64_t *stride)
+                                     const int64_t *stride, uint32_t box_rows)
 {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)S, (cuuint64_t)heads, (cuuint64_t)B};
     const cuuint64_t strides[3] = {(cuuint64_t)stride[2] * 2, (cuuint64_t)stride[1] * 2, (cuuint64_t)stride[0] * 2};
-    const cuuint32_t box[4] = {64, 128, 1, 1};
+    const cuuint32_t box[4] = {64, box_rows, 1, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
     return fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims,
               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,

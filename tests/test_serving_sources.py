@@ -1,0 +1,62 @@
+"""Rules that the serving kernels' sources have to keep: dependent launch, tensor memory, registers that roles share out.
+What breaks them is a wait that never ends or stale data, which no test provokes on a GPU."""
+import os
+import re
+
+import pytest
+
+from paper_2602_02071_b200 import build
+
+SRC = {n: open(os.path.join(build.CSRC, n)).read() for n in sorted(os.listdir(build.CSRC)) if n.endswith((".cu", ".cuh"))}
+CODE = {n: re.sub(r"//[^\n]*", "", s) for n, s in SRC.items()}
+NEW = ["baps_attention_window.cuh", "baps_kv_append.cuh", "baps_kv_attention.cuh", "baps_kv_pages.cuh"]
+
+
+def kernels():
+    """(name, body) of every __global__ function of the serving files."""
+    for n in NEW:
+        for m in re.finditer(r"__global__\s+void\s+(?:__launch_bounds__\((?:[^()]|\([^()]*\))*\)\s*)?(\w+)\(", CODE[n]):
+            yield m.group(1), CODE[n][m.start():CODE[n].index("\n}", m.start())]
+
+
+KERNELS = dict(kernels())
+
+
+def test_all_kernels_are_found():
+    assert set(KERNELS) == {"window_attention_kernel", "kv_append_kernel", "kv_attention_kernel", "kv_join_kernel", "kv_fork_plan_kernel",
+                            "kv_fork_rows_kernel", "kv_compact_count_kernel", "kv_compact_lists_kernel", "kv_compact_move_kernel"}
+    assert sum(c.count("__global__") for n, c in CODE.items() if n in NEW) == len(KERNELS)
+
+
+@pytest.mark.parametrize("name", sorted(KERNELS))
+def test_every_kernel_waits_for_the_kernel_ahead_before_it_reads(name):
+    body = KERNELS[name]
+    assert body.count("await_previous_kernel(") == 1 and body.count("allow_next_kernel()") == 1
+    wait = body.index("await_previous_kernel(")
+    # no caller memory ahead of the wait: parameters are only read through pointers behind it
+    assert not re.search(r"p\.\w+\s*\[|\*p\.|\*reinterpret_cast", body[body.index("{"):wait])
+
+
+def test_tensor_memory_is_taken_between_the_kernel_ahead_and_the_next_one():
+    body = KERNELS["window_attention_kernel"]
+    assert body.index("await_previous_kernel()") < body.index("tmem_alloc(") < body.index("allow_next_kernel()") < body.index("tmem_dealloc(")
+    # what three CTAs of an SM hold fits
+    code = CODE["baps_attention_window.cuh"]
+    assert re.search(r"kTmemCols = kKeys == 64 \? 128 : 256 \* kStreams", code) and re.search(r"kCtasPerSm = kKeys == 64 \? 3 : 1", code)
+
+
+def test_the_cache_kernels_wait_for_nothing_but_their_own_copies():
+    for name, body in KERNELS.items():
+        if name != "window_attention_kernel":
+            assert "mbar_" not in body and "while" not in body, name
+
+
+def test_the_windowed_kernel_has_the_registers_that_its_roles_share_out():
+    code = CODE["baps_attention_window.cuh"]
+    assert re.findall(r'setmaxnreg\.\w+\.sync\.aligned\.u32 %0;" ::"n"\(kTcSplit\.(few|many)\)', code) == ["few", "many"]
+    assert code.count("setmaxnreg.") == 2 and code.index("!has_registers_for<") < code.index("return launch_kernel(")
+    build.build()
+    log = open(os.path.join(os.path.dirname(build.LIB), "build.log")).read()
+    used = re.findall(r"Compiling entry function '\w*window_attention_kernelI\w*Li128ELi2ELi128E\w*'.*?Used (\d+) registers", log, re.S)
+    # 128 threads at 64 and 512 at 104 out of 640 at what the kernel was compiled to
+    assert len(used) == 2 and all(128 * 64 + 512 * 104 <= 640 * int(r) for r in used)
