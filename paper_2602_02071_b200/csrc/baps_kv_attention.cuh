@@ -249,7 +249,7 @@ kv_attention_kernel(const KvAttnParams p)
         const int total = s_pre[p.B] * heads;                              // (fits: checked on the host)
         per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, kKvMinTiles);
         w0 = (int)min((int64_t)blockIdx.x * per, (int64_t)total);
-        w1 = min(w0 + per, total);
+        w1 = (int)min((int64_t)w0 + per, (int64_t)total);
         if (tid == 0) p.desc[blockIdx.x] = make_int2(-1, 0);
         if (w0 >= w1) return;
     }

@@ -141,17 +141,23 @@ kv_fork_plan_kernel(const KvForkParams p)
     }
     const int need = min(base, p.most);
     int found = 0;
-    // (four pages per thread and step; 16-byte loads need the caller's array to be aligned, which it is)
-    for (int i0 = 0; i0 < p.pool.n_pages && found < need; i0 += 4096) {
-        const int i = i0 + 4 * (int)threadIdx.x;
-        int r[4] = {1, 1, 1, 1};
+    // (four pages per thread and step, the next step's on their way; the array is aligned for 16-byte loads)
+    auto load = [&](int64_t i) {
+        int4 v = make_int4(1, 1, 1, 1);
         if (i + 3 < p.pool.n_pages) {
-            const int4 v = *reinterpret_cast<const int4 *>(p.refs + i);
-            r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+            v = *reinterpret_cast<const int4 *>(p.refs + i);
         } else {
-            for (int k = 0; k < 4; ++k)
-                if (i + k < p.pool.n_pages) r[k] = p.refs[i + k];
+            if (i < p.pool.n_pages) v.x = p.refs[i];
+            if (i + 1 < p.pool.n_pages) v.y = p.refs[i + 1];
+            if (i + 2 < p.pool.n_pages) v.z = p.refs[i + 2];
         }
+        return v;
+    };
+    int4 now = load(4 * (int)threadIdx.x);
+    for (int64_t i0 = 0; i0 < p.pool.n_pages && found < need; i0 += 4096) {
+        const int i = (int)i0 + 4 * (int)threadIdx.x;
+        const int r[4] = {now.x, now.y, now.z, now.w};
+        now = load((int64_t)i + 4096);
         int free_here = 0, sum;
 #pragma unroll
         for (int k = 0; k < 4; ++k) free_here += r[k] == 0;

@@ -92,6 +92,16 @@ def test_fork_of_many_rows():
     check_fork(pool(n_pages, 1, page, 64, 1), page, table, lengths, refs, parents, 5)
 
 
+def test_fork_that_looks_far_for_free_pages():
+    """All free pages stand behind 40000 used ones."""
+    page, n_pages = 16, 40100
+    table, lengths, refs = batch(4, 5, page, 60, 3, most=70)
+    refs = refs + [1] * (n_pages - 60 - 37) + [0] * 37
+    for i in range(60):
+        refs[i] = max(refs[i], 1)
+    check_fork(pool(n_pages, 1, page, 64, 1), page, table, lengths, refs, [0, 1, 2, 3, 0, 1, 2, 0], 30)
+
+
 def check_compact(state, table, refs):
     before = [t.clone() for t in state]
     got = binding.baps_kv_compact(binding.KvCache(*state), ints(table).view(len(table), len(table[0]) if table else 0), ints(refs))
