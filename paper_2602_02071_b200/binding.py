@@ -352,7 +352,10 @@ def baps_attention_restart_rates_static(q, k, v, *, causal: bool, out: torch.Ten
 # allocated from a tensor of their kind (new_empty, 1.7 us; torch.empty with a type and a device, 2.3).
 
 _DTYPE16 = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+_U8, _I32, _F32 = torch.uint8, torch.int32, torch.float32
 _device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_empty_like = torch.empty_like
 
 
 def _dtype16(t: torch.Tensor, name: str) -> int:
@@ -369,7 +372,7 @@ def _stride3(t: torch.Tensor, like: torch.Tensor, shape, name: str):
     """Strides (elements) of the leading three dimensions of a tensor of contiguous rows; where a dimension has one
     element only, its stride does not matter and may be anything."""
     st = t.stride()
-    if t.dtype != like.dtype or t.shape != shape or t.device != like.device or st[3] != 1:
+    if st[3] != 1 or t.dtype != like.dtype or t.shape != shape or t.get_device() != like.get_device():
         raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
     a, b, c, _ = shape
     return (st[0] if a > 1 else 8, st[1] if b > 1 else 8, st[2] if c > 1 else 8)
@@ -377,14 +380,14 @@ def _stride3(t: torch.Tensor, like: torch.Tensor, shape, name: str):
 
 def _stride2(t: torch.Tensor, like: torch.Tensor, shape, name: str):
     st = t.stride()
-    if t.dtype != like.dtype or t.shape != shape or t.device != like.device or st[2] != 1:
+    if st[2] != 1 or t.dtype != like.dtype or t.shape != shape or t.get_device() != like.get_device():
         raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
     return (st[0] if shape[0] > 1 else 8, st[1] if shape[1] > 1 else 8)
 
 
-def _buffer(t: torch.Tensor, dtype, device, shape, name: str) -> int:
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _buffer(t: torch.Tensor, dtype, index: int, shape, name: str) -> int:
+    if t.dtype != dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}")
     return t.data_ptr()
 
 
@@ -406,17 +409,17 @@ def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0,
     visible; causal, plain softmax.  q [B,H,S,D], k, v [B,Hkv,S,D] bfloat16 or float16, any strides with contiguous rows
     (for example a [B,S,heads,D] projection seen as [B,heads,S,D]).  ``lengths`` (int32 [B]): tokens of each
     sequence of a padded batch; rows behind them are left as they are in ``out`` and ``lse`` (float32 [B,H,S])."""
-    code = _dtype16(q, "q")
+    code, index = _dtype16(q, "q"), q.get_device()
     B, H, Hkv, S, D = _attn_shapes(q, k, v)
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty_like(q)
     qs, ks = q.shape, k.shape
     st = _pack("12q", *_stride3(q, q, qs, "q"), *_stride3(k, q, ks, "k"), *_stride3(v, q, ks, "v"), *_stride3(out, q, qs, "out"))
     status = load().baps_attention_window_fwd(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-        None if lse is None else _buffer(lse, torch.float32, q.device, (B, H, S), "lse"),
-        None if lengths is None else _buffer(lengths, torch.int32, q.device, (B,), "lengths"), st, B, H, Hkv, S, D,
-        _window(window), int(sinks), float(scale), code, _stream())
+        None if lse is None else _buffer(lse, _F32, index, (B, H, S), "lse"),
+        None if lengths is None else _buffer(lengths, _I32, index, (B,), "lengths"), st, B, H, Hkv, S, D,
+        _window(window), int(sinks), float(scale), code, _raw_stream(index))
     if status:
         _check("baps_attention_window_fwd", status)
     return out
@@ -428,17 +431,16 @@ class KvCache:
     __slots__ = ("k", "v", "k_scale", "v_scale", "struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        shape, device = k.shape, k.device
-        if len(shape) != 4 or not k.is_cuda:
-            raise ValueError("k: expected CUDA codes [n_pages, Hkv, page, D]")
-        if k.dtype != torch.uint8 or v.dtype != torch.uint8 or v.shape != shape or v.device != device or \
+        shape, index, pages = k.shape, k.get_device(), k_scale.shape
+        if len(shape) != 4 or index < 0 or k.dtype != _U8 or v.dtype != _U8 or v.shape != shape or v.get_device() != index or \
                 not (k.is_contiguous() and v.is_contiguous()):
-            raise ValueError("k, v: expected contiguous uint8 CUDA tensors of one shape")
-        pages = shape[:2]
+            raise ValueError("k, v: expected contiguous uint8 CUDA tensors of one shape [n_pages, Hkv, page, D]")
+        if pages != shape[:2] or v_scale.shape != pages or k_scale.dtype != _F32 or v_scale.dtype != _F32 or \
+                k_scale.get_device() != index or v_scale.get_device() != index or not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+            raise ValueError("k_scale, v_scale: expected contiguous float32 tensors [n_pages, Hkv] on the codes' device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         # baps_kv_cache
-        self.struct = _pack("4Q4i", k.data_ptr(), v.data_ptr(), _buffer(k_scale, torch.float32, device, pages, "k_scale"),
-                            _buffer(v_scale, torch.float32, device, pages, "v_scale"), *shape)
+        self.struct = _pack("4Q4i", k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *shape)
 
     @classmethod
     def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":
@@ -446,26 +448,26 @@ class KvCache:
         scales = [torch.ones((n_pages, Hkv), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(*codes, *scales)
 
-    def here(self) -> torch.device:
-        """The cache's device, which has to be the current one."""
-        if self.k.get_device() != _device():
+    def here(self) -> int:
+        """Number of the cache's device, which has to be the current one."""
+        index = self.k.get_device()
+        if index != _device():
             raise ValueError(f"the cache is on {self.k.device}, the current device is cuda:{_device()}")
-        return self.k.device
+        return index
 
 
 def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_new: Optional[int] = None) -> None:
     """Write new tokens into the cache: k_new, v_new [n,Hkv,D] bfloat16 or float16 (contiguous rows, any strides), tokens
     starts[b] .. starts[b+1]-1 behind the lengths[b] that sequence b holds, in the pages of its row of ``table`` (int32
     [B,width]).  ``max_new``: most tokens of one sequence (default: all of them).  ``lengths`` is not changed."""
-    code = _dtype16(k_new, "k_new")
-    device = cache.here()
+    code, index = _dtype16(k_new, "k_new"), cache.here()
     n, (_, Hkv, _, D) = k_new.shape[0], cache.k.shape
     B, width = table.shape
     st = _pack("4q", *_stride2(k_new, k_new, (n, Hkv, D), "k_new"), *_stride2(v_new, k_new, (n, Hkv, D), "v_new"))
     status = load().baps_kv_append(
-        cache.struct, k_new.data_ptr(), v_new.data_ptr(), st, n, _buffer(starts, torch.int32, device, (B + 1,), "starts"),
-        _buffer(lengths, torch.int32, device, (B,), "lengths"), _buffer(table, torch.int32, device, (B, width), "table"), width, B,
-        n if max_new is None else min(int(max_new), n), code, _stream())
+        cache.struct, k_new.data_ptr(), v_new.data_ptr(), st, n, _buffer(starts, _I32, index, (B + 1,), "starts"),
+        _buffer(lengths, _I32, index, (B,), "lengths"), _buffer(table, _I32, index, (B, width), "table"), width, B,
+        n if max_new is None else min(int(max_new), n), code, _raw_stream(index))
     if status:
         _check("baps_kv_append", status)
 
@@ -488,9 +490,7 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     strides), query t at position lengths[b]-T+t, T <= 16.  Returns out, or (out, lse float32 [B,H,T]) if ``want_lse``.
     ``workspace``: a uint8 tensor of ``kv_attention_workspace`` bytes, allocated here if not given; calls that may run at
     the same time need one each."""
-    code = _dtype16(q, "q")
-    device = cache.here()
-    shape = q.shape
+    code, index, shape = _dtype16(q, "q"), cache.here(), q.shape
     B, H, T, D = shape
     _, Hkv, page, Dc = cache.k.shape
     rows, width = table.shape
@@ -498,26 +498,26 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     if D != Dc or rows != B:
         raise ValueError("q does not match the cache, or table is not [B,width]")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty_like(q)
     if lse is not None:
-        lse_ptr = _buffer(lse, torch.float32, device, (B, H, T), "lse")
+        lse_ptr = _buffer(lse, _F32, index, (B, H, T), "lse")
     elif want_lse:
         lse = cache.k_scale.new_empty((B, H, T))
         lse_ptr = lse.data_ptr()
     else:
         lse_ptr = None
     if workspace is None:
-        n = _attention_workspace(_device(), B, H, Hkv, T, D, page, width, window, sinks)
+        n = _attention_workspace(index, B, H, Hkv, T, D, page, width, window, sinks)
         ws_ptr = (workspace := cache.k.new_empty((n,))).data_ptr() if n else None
-    elif workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous():
+    elif workspace.dtype != _U8 or workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor on q's device")
     else:
         n, ws_ptr = workspace.numel(), workspace.data_ptr()
     st = _pack("6q", *_stride3(q, q, shape, "q"), *_stride3(out, q, shape, "out"))
     status = load().baps_kv_attention(
-        q.data_ptr(), out.data_ptr(), lse_ptr, cache.struct, _buffer(table, torch.int32, device, (B, width), "table"), width,
-        _buffer(lengths, torch.int32, device, (B,), "lengths"), st, B, H, T, window, sinks, float(scale), code, ws_ptr, n,
-        _stream())
+        q.data_ptr(), out.data_ptr(), lse_ptr, cache.struct, _buffer(table, _I32, index, (B, width), "table"), width,
+        _buffer(lengths, _I32, index, (B,), "lengths"), st, B, H, T, window, sinks, float(scale), code, ws_ptr, n,
+        _raw_stream(index))
     if status:
         _check("baps_kv_attention", status)
     return (out, lse) if want_lse else out
@@ -534,16 +534,18 @@ def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int 
     pages shared, last pages copied for all children of a parent but the first, pages outside the window let go, free pages
     (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a
     row that found no room has length -1."""
-    device, i32 = cache.here(), torch.int32
+    index = cache.here()
     rows, width = table.shape
     n_pages, (new_rows,) = cache.k.shape[0], parents.shape
-    ptrs = (_buffer(table, i32, device, (rows, width), "table"), _buffer(lengths, i32, device, (rows,), "lengths"),
-            _buffer(refs, i32, device, (n_pages,), "refs"), _buffer(parents, i32, device, (new_rows,), "parents"))
-    new, new_lengths, new_refs = table.new_empty((new_rows, width)), torch.empty_like(parents), torch.empty_like(refs)
+    ptrs = (_buffer(table, _I32, index, (rows, width), "table"), _buffer(lengths, _I32, index, (rows,), "lengths"),
+            _buffer(refs, _I32, index, (n_pages,), "refs"), _buffer(parents, _I32, index, (new_rows,), "parents"))
+    new = _empty_like(table) if new_rows == rows else table.new_empty((new_rows, width))
+    new_lengths, new_refs = _empty_like(parents), _empty_like(refs)
     n = _pages_workspace(new_rows, n_pages)
     ws = cache.k.new_empty((n,))
     status = load().baps_kv_fork(cache.struct, ptrs[0], ptrs[1], rows, ptrs[2], ptrs[3], new_rows, width, int(reserve), _window(window),
-                                 int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(), ws.data_ptr(), n, _stream())
+                                 int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(), ws.data_ptr(), n,
+                                 _raw_stream(index))
     if status:
         _check("baps_kv_fork", status)
     return new, new_lengths, new_refs
@@ -551,15 +553,15 @@ def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int 
 
 def baps_kv_compact(cache: KvCache, table, refs):
     """Move the pages in use to the front of the pool.  Returns (new_table, new_refs, page_map, n_live), all int32."""
-    device, i32 = cache.here(), torch.int32
+    index = cache.here()
     rows, width = table.shape
     n_pages = cache.k.shape[0]
-    table_ptr, refs_ptr = _buffer(table, i32, device, (rows, width), "table"), _buffer(refs, i32, device, (n_pages,), "refs")
-    new, new_refs, page_map, n_live = torch.empty_like(table), torch.empty_like(refs), torch.empty_like(refs), refs.new_empty((1,))
+    table_ptr, refs_ptr = _buffer(table, _I32, index, (rows, width), "table"), _buffer(refs, _I32, index, (n_pages,), "refs")
+    new, new_refs, page_map, n_live = _empty_like(table), _empty_like(refs), _empty_like(refs), refs.new_empty((1,))
     n = _pages_workspace(0, n_pages)
     ws = cache.k.new_empty((n,))
     status = load().baps_kv_compact(cache.struct, table_ptr, rows, width, refs_ptr, new.data_ptr(), new_refs.data_ptr(),
-                                    page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(), n, _stream())
+                                    page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(), n, _raw_stream(index))
     if status:
         _check("baps_kv_compact", status)
     return new, new_refs, page_map, n_live
