@@ -731,12 +731,15 @@ kv_join_kernel(const KvAttnParams p)
 
 // Rows of a kv head go to a CTA 8 or 16 (D = 64: up to 32) at a time, as many as its registers hold; more are items of their own,
 // which CTAs work on at about the same time, so that most of what they read again comes from L2.
-// Short contexts: every sequence and kv head to a cluster of its own, of as many CTAs (up to eight) as still run all at the same
-// time, or to one CTA, if that gives a CTA 16 tiles at most (most_tiles: what a sequence can have, by its row of the table
-// and the window).  Measured against the even cut (32 / 8 heads of 128, clusters first): one sequence of 2000 tokens 7.9 us, 10.1; of 8000
-// 12.7, 14.0; of 16000 18.7, 16.2; 32 of 1000 15.1, 22.8; 128 of 1000 50.8, 60.5; 300 of 500 83, 101.
+// Sequences and kv heads ("items") that are short, or cut to one length by a window, go to a cluster of up to eight CTAs each,
+// as many as still run all at the same time, or to one CTA: one launch, nothing to join through memory, no CTA with two items.
+// That is taken where a CTA gets few enough tiles for it (most_tiles: what an item can have, by the table's width and the window):
+//   24 for an item to itself, 16 in a cluster, 36 where the window sets the length and the clusters fill four fifths of the machine.
+// Measured against the even cut, us (clusters first; 32 / 8 heads of 128 unless said): one sequence of 2000 tokens 7.1, 10.1; of 8000 12.7, 14.0; of
+// 12000 (24 tiles) 15.0, 12.7; six of up to 8000 (21 tiles, lengths differ) 22.3, 18.2; 30 of 1500 (a CTA each) 16.5, 21.8; 60 of 1500 32.2, 38.8;
+// 32 with window 4096, four queries each: 16 / 4 heads of 64 20.7, 26.1; of 128 32.6, 39.0.
 struct KvShape { int tiles, groups, ctas, cluster; };
-static inline KvShape kv_shape(int R, int D, int64_t items = 0, int64_t most_tiles = 0)
+static inline KvShape kv_shape(int R, int D, int64_t items, int64_t most_tiles, bool by_window)
 {
     KvShape s;
     s.tiles = R <= 8 ? 1 : R <= 16 || D == 128 ? 2 : 4;
@@ -744,17 +747,20 @@ static inline KvShape kv_shape(int R, int D, int64_t items = 0, int64_t most_til
     s.ctas = num_sms() * (D == 64 && s.tiles < 4 ? 3 : 2);
     s.cluster = 0;
     items *= s.groups;
-    if (most_tiles > 0)
-        for (int c = 1; c <= 8; c *= 2)
-            if ((c == 1 || items * c <= s.ctas) && (most_tiles + c - 1) / c <= 16) s.cluster = c;
+    for (int c = 1; c <= 8; ++c) {
+        const int64_t each = (most_tiles + c - 1) / c;
+        const bool fits = items * c <= s.ctas, full = fits && 5 * items * c >= 4 * s.ctas;
+        if (c == 1 ? each <= 24 : fits && (each <= 16 || (by_window && full && each <= 36))) s.cluster = c;
+    }
     return s;
 }
-// Tiles that a sequence can have.
-static inline int64_t kv_most_tiles(int page, int table_width, int T, int window, int sinks)
+// Tiles that a sequence can have by its row of the table, and by the window.
+static inline int64_t kv_held_tiles(int page, int table_width) { return ((int64_t)table_width * page + kKvTile - 1) / kKvTile; }
+static inline int64_t kv_seen_tiles(int T, int window, int sinks) { return ((int64_t)window + T) / kKvTile + sinks / kKvTile + 4; }
+static inline KvShape kv_shape_of(int B, int Hkv, int R, int D, int page, int table_width, int T, int window, int sinks)
 {
-    const int64_t held = ((int64_t)table_width * page + kKvTile - 1) / kKvTile;
-    const int64_t seen = ((int64_t)window + T) / kKvTile + sinks / kKvTile + 4;
-    return held < seen ? held : seen;
+    const int64_t held = kv_held_tiles(page, table_width), seen = kv_seen_tiles(T, window, sinks);
+    return kv_shape(R, D, (int64_t)B * Hkv, held < seen ? held : seen, seen < held);
 }
 // Bytes: part_o, part_ml, desc
 static inline size_t kv_workspace(const KvShape &s, int D)

@@ -130,7 +130,7 @@ size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page
     if (B <= 0 || B > kKvMaxB || H <= 0 || Hkv <= 0 || H % Hkv != 0 || T <= 0 || T > 16 || (D != 64 && D != 128)) return 0;
     if ((page != 16 && page != 32 && page != 64 && page != 128) || table_width <= 0 || window < 1 || sinks < 0) return 0;
     if ((int64_t)T * (H / Hkv) > 65536) return 0;
-    return kv_workspace(kv_shape(T * (H / Hkv), D, (int64_t)B * Hkv, kv_most_tiles(page, table_width, T, window, sinks)), D);
+    return kv_workspace(kv_shape_of(B, Hkv, T * (H / Hkv), D, page, table_width, T, window, sinks), D);
 }
 
 baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_kv_cache *cache, const int32_t *table,
@@ -154,8 +154,8 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
         if (!strides_ok(strides, 6)) return BAPS_ERR_INVALID_ARG;
         for (int i = 0; i < 6; ++i) s[i] = strides[i];
     }
-    const int64_t tiles = kv_most_tiles(cache->page, table_width, T, window, sinks);
-    const KvShape shape = kv_shape(T * (H / cache->Hkv), D, (int64_t)B * cache->Hkv, tiles);
+    const int64_t held = kv_held_tiles(cache->page, table_width), seen = kv_seen_tiles(T, window, sinks), tiles = held < seen ? held : seen;
+    const KvShape shape = kv_shape_of(B, cache->Hkv, T * (H / cache->Hkv), D, cache->page, table_width, T, window, sinks);
     const size_t need = kv_workspace(shape, D);
     if (need > 0 && (!workspace || workspace_bytes < need)) return BAPS_ERR_INVALID_ARG;
     // tiles of the whole call are a 32-bit count
