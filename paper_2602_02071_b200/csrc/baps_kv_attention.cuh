@@ -8,24 +8,26 @@
 // after they have been summed.  The scales are applied in float32; O~ is kept in units of a value scale that is followed
 // where a page's leaves [unit / 64, unit].
 //
-// What bounds it: the bytes of K and V, one per element.  mma.sync, not tcgen05: the codes have to be widened in registers
-// on the way, and a CTA has 8 to 64 rows of queries, where a tcgen05 tile has 128.  K and V are the operand with 16
-// rows and the queries the one with 8 columns (S^T = K Q^T, O^T = V^T P^T), so that eight query rows waste nothing: a product of 16 x 8 x 16
-// takes 8 cycles of a scheduler's tensor core and covers 256 codes.  (Queries as the 16 rows: twice the products, 4.3 TB/s on the long
-// decoding batch.  E4M3 operands, q and weights in two parts each: mma.sync m16n8k32 is carried out as fp16 products
-// with both operands widened every time, 26 cycles instead of 5 once they change, 4.6 TB/s.)
+// What bounds it: the bytes of K and V, one per element: 48 sequences of 8192 to 32768 tokens, 32 / 8 heads of 128, pages of 64,
+// 298 us, 6.7 TB/s.  mma.sync, not tcgen05: the codes have to be widened in registers on the way, and a CTA has 8 to 32 rows of
+// queries, where a tcgen05 tile has 128.  K and V are the operand with 16 rows and the queries the one with 8 columns
+// (S^T = K Q^T, O^T = V^T P^T), so that eight query rows waste nothing: a product of 16 x 8 x 16 takes 8 cycles of a scheduler's
+// tensor core and covers 256 codes.  (Queries as the 16 rows: twice the products, 471 us.  E4M3 operands, q and weights in two
+// parts each: mma.sync m16n8k32 is carried out as fp16 products with both operands widened every time, 26 cycles instead
+// of 5 once they change, 433 us.)
 //
 // Work is cut evenly whatever the lengths: the 64-key tiles of all sequences and kv heads, visible ones only, in one row;
 // CTA i takes an equal share.  What a CTA does of a sequence and head that is not whole goes to the workspace and a
-// second kernel joins it, in the order of the CTAs.  Each of a CTA's four warps takes every fourth 32 keys of its share for 8 to 32
-// rows of queries and keeps m, l and O~ in registers; they are joined through shared memory where a sequence and head
-// ends.  A warp copies its own keys (16 bytes per lane, two to four steps ahead), so that no warp waits for another before that.
+// second kernel joins it, in the order of the CTAs.  (Short ones, and those that a window cuts to one length, go to clusters:
+// kv_shape.)  Each of a CTA's four warps takes every fourth 32 keys of its share for 8 to 32 rows of queries and keeps
+// m, l and O~ in registers; they are joined through shared memory where a sequence and head ends.  A warp copies its own
+// keys (16 bytes per lane, two to four steps ahead), so that no warp waits for another before that.
 // (Before: a producer warp and TMA boxes into a ring of tiles.  The same 6.5 TB/s for pages of 64 tokens, but a box takes
 // about 120 cycles of the SM's unit however small it is, 414 us for 309 with pages of 16; and a fifth warp costs a fifth of
 // the registers.)
 //
-// Fragments (g = lane / 4, t = lane % 4).  The order of keys within 16 is free: place i is key key_of(i), chosen so that neither the
-// reads of K nor those of V, which ldmatrix transposes byte by byte, meet a bank twice.
+// Fragments (g = lane / 4, t = lane % 4).  The order of keys within 16 is free: place i is key key_of(i), chosen so that
+// neither the reads of K nor those of V, which ldmatrix transposes byte by byte, meet a bank twice.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

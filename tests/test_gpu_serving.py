@@ -143,6 +143,40 @@ def test_a_step_in_a_graph_runs_many_steps():
     cache_test.check(qkv[:, :H, None].cpu(), state, table.cpu(), lengths.cpu(), serving.NONE, 0, got=(out, lse))
 
 
+def test_calls_and_graphs_on_several_streams_at_once():
+    """Eager calls and captured ones of every form run beside each other: each has its workspace, results do not move."""
+    jobs = []
+    for i, (B, H, Hkv, T, D, page, lengths, window) in enumerate([
+            (3, 8, 2, 1, 128, 64, [9000, 3000, 12000], serving.NONE), (2, 16, 4, 4, 64, 16, [9000, 20000], 4096),
+            (4, 8, 1, 1, 128, 16, [100, 2000, 30, 700], serving.NONE)]):
+        q, state, table, n = cache_test.make(B, H, Hkv, T, D, page, lengths, torch.bfloat16, seed=i, window=window)
+        args = q.cuda(), binding.KvCache(*state), table.cuda(), n.cuda()
+        jobs.append(lambda args=args, window=window: binding.baps_kv_attention(*args, window=window))
+    for i, (B, H, Hkv, S, D) in enumerate([(2, 8, 2, 2000, 128), (2, 8, 2, 3000, 64), (1, 2, 1, 300, 128)]):
+        args = window_test.make(B, H, Hkv, S, D, torch.float16, i)
+        jobs.append(lambda args=args: binding.baps_attention_window_fwd(*args, window=700, sinks=5))
+    want = [f().clone() for f in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    graphs = []
+    for f, s in zip(jobs, streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = f()
+        graphs.append((graph, out))
+    for _ in range(20):
+        eager = []
+        for f, (graph, _), s in zip(jobs, graphs, streams):
+            with torch.cuda.stream(s):
+                eager.append(f())
+                graph.replay()
+                eager.append(f())
+        torch.cuda.synchronize()
+        for i, w in enumerate(want):
+            assert torch.equal(eager[2 * i], w) and torch.equal(eager[2 * i + 1], w) and torch.equal(graphs[i][1], w), i
+    binding.poll_async_error()
+
+
 def test_an_expired_wait_of_the_windowed_attention_is_reported():
     """In the build whose waits end after 1 ms, with one tile load left out: nothing is stored, the status says so, the next
     call is right.  One and two query tiles per CTA, heads of 64, a padded batch."""
