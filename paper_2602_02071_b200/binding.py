@@ -8,9 +8,7 @@ is missing the import of the library fails loudly -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
-import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -347,59 +345,29 @@ def baps_attention_restart_rates_static(q, k, v, *, causal: bool, out: torch.Ten
 
 # ---- serving: windowed prompts, the 8-bit cache, its attention and its pages -----------------------------------------
 #
-# The smallest of these calls take a few microseconds on the device, so the checks are written to be cheap: one condition
-# per tensor, structures and strides handed over as packed bytes (a ctypes structure takes 1 us to fill), outputs
-# allocated from a tensor of their kind (new_empty, 1.7 us; torch.empty with a type and a device, 2.3).
+# The smallest of these calls take a few microseconds on the device, less than the same checks take in Python.  So tensors are
+# checked, outputs allocated and pointers passed by an extension module built from csrc/serving_marshal.c, which calls the
+# functions of the library that load() returns.
 
-_DTYPE16 = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
-_U8, _I32, _F32 = torch.uint8, torch.int32, torch.float32
-_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_empty_like = torch.empty_like
+_serving = None
+_SERVING_CALLS = ["baps_attention_window_fwd", "baps_kv_append", "baps_kv_attention", "baps_kv_attention_workspace", "baps_kv_fork",
+                  "baps_kv_compact", "baps_kv_pages_workspace"]
 
 
-def _dtype16(t: torch.Tensor, name: str) -> int:
-    """Code of the type of a 16-bit CUDA tensor on the current device (the library launches on that one)."""
-    code = _DTYPE16.get(t.dtype)
-    if code is None or not t.is_cuda:
-        raise ValueError(f"{name}: expected a bfloat16 or float16 CUDA tensor")
-    if t.get_device() != _device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_device()}")
-    return code
-
-
-def _stride3(t: torch.Tensor, like: torch.Tensor, shape, name: str):
-    """Strides (elements) of the leading three dimensions of a tensor of contiguous rows; where a dimension has one
-    element only, its stride does not matter and may be anything."""
-    st = t.stride()
-    if st[3] != 1 or t.dtype != like.dtype or t.shape != shape or t.get_device() != like.get_device():
-        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
-    a, b, c, _ = shape
-    return (st[0] if a > 1 else 8, st[1] if b > 1 else 8, st[2] if c > 1 else 8)
-
-
-def _stride2(t: torch.Tensor, like: torch.Tensor, shape, name: str):
-    st = t.stride()
-    if st[2] != 1 or t.dtype != like.dtype or t.shape != shape or t.get_device() != like.get_device():
-        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(shape)} with contiguous rows on {like.device}")
-    return (st[0] if shape[0] > 1 else 8, st[1] if shape[1] > 1 else 8)
-
-
-def _buffer(t: torch.Tensor, dtype, index: int, shape, name: str) -> int:
-    if t.dtype != dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}")
-    return t.data_ptr()
+def _marshal():
+    global _serving
+    if _serving is None:
+        from . import _serving as module
+        lib = load()
+        module.bind((torch.bfloat16, torch.float16, torch.float32, torch.int32, torch.uint8, torch.empty_like, torch._C._cuda_getDevice,
+                     torch._C._cuda_getCurrentRawStream, _check),
+                    tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _SERVING_CALLS))
+        _serving = module
+    return _serving
 
 
 def _window(window: Optional[int]) -> int:
-    return ALL_KEYS if window is None else min(int(window), ALL_KEYS)
-
-
-def _pack(fmt: str, *values) -> bytes:
-    try:
-        return struct.pack(fmt, *values)
-    except struct.error as e:
-        raise ValueError(f"a size is out of range: {e}") from None
+    return ALL_KEYS if window is None else window
 
 
 def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0, scale: float = 0.0,
@@ -409,20 +377,7 @@ def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0,
     visible; causal, plain softmax.  q [B,H,S,D], k, v [B,Hkv,S,D] bfloat16 or float16, any strides with contiguous rows
     (for example a [B,S,heads,D] projection seen as [B,heads,S,D]).  ``lengths`` (int32 [B]): tokens of each
     sequence of a padded batch; rows behind them are left as they are in ``out`` and ``lse`` (float32 [B,H,S])."""
-    code, index = _dtype16(q, "q"), q.get_device()
-    B, H, Hkv, S, D = _attn_shapes(q, k, v)
-    if out is None:
-        out = _empty_like(q)
-    qs, ks = q.shape, k.shape
-    st = _pack("12q", *_stride3(q, q, qs, "q"), *_stride3(k, q, ks, "k"), *_stride3(v, q, ks, "v"), *_stride3(out, q, qs, "out"))
-    status = load().baps_attention_window_fwd(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-        None if lse is None else _buffer(lse, _F32, index, (B, H, S), "lse"),
-        None if lengths is None else _buffer(lengths, _I32, index, (B,), "lengths"), st, B, H, Hkv, S, D,
-        _window(window), int(sinks), float(scale), code, _raw_stream(index))
-    if status:
-        _check("baps_attention_window_fwd", status)
-    return out
+    return (_serving or _marshal()).window(q, k, v, out, lse, lengths, _window(window), sinks, scale)
 
 
 class KvCache:
@@ -431,16 +386,8 @@ class KvCache:
     __slots__ = ("k", "v", "k_scale", "v_scale", "struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        shape, index, pages = k.shape, k.get_device(), k_scale.shape
-        if len(shape) != 4 or index < 0 or k.dtype != _U8 or v.dtype != _U8 or v.shape != shape or v.get_device() != index or \
-                not (k.is_contiguous() and v.is_contiguous()):
-            raise ValueError("k, v: expected contiguous uint8 CUDA tensors of one shape [n_pages, Hkv, page, D]")
-        if pages != shape[:2] or v_scale.shape != pages or k_scale.dtype != _F32 or v_scale.dtype != _F32 or \
-                k_scale.get_device() != index or v_scale.get_device() != index or not (k_scale.is_contiguous() and v_scale.is_contiguous()):
-            raise ValueError("k_scale, v_scale: expected contiguous float32 tensors [n_pages, Hkv] on the codes' device")
+        self.struct = (_serving or _marshal()).cache_struct(k, v, k_scale, v_scale)          # baps_kv_cache
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        # baps_kv_cache
-        self.struct = _pack("4Q4i", k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *shape)
 
     @classmethod
     def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":
@@ -448,39 +395,18 @@ class KvCache:
         scales = [torch.ones((n_pages, Hkv), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(*codes, *scales)
 
-    def here(self) -> int:
-        """Number of the cache's device, which has to be the current one."""
-        index = self.k.get_device()
-        if index != _device():
-            raise ValueError(f"the cache is on {self.k.device}, the current device is cuda:{_device()}")
-        return index
-
 
 def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_new: Optional[int] = None) -> None:
     """Write new tokens into the cache: k_new, v_new [n,Hkv,D] bfloat16 or float16 (contiguous rows, any strides), tokens
     starts[b] .. starts[b+1]-1 behind the lengths[b] that sequence b holds, in the pages of its row of ``table`` (int32
     [B,width]).  ``max_new``: most tokens of one sequence (default: all of them).  ``lengths`` is not changed."""
-    code, index = _dtype16(k_new, "k_new"), cache.here()
-    n, (_, Hkv, _, D) = k_new.shape[0], cache.k.shape
-    B, width = table.shape
-    st = _pack("4q", *_stride2(k_new, k_new, (n, Hkv, D), "k_new"), *_stride2(v_new, k_new, (n, Hkv, D), "v_new"))
-    status = load().baps_kv_append(
-        cache.struct, k_new.data_ptr(), v_new.data_ptr(), st, n, _buffer(starts, _I32, index, (B + 1,), "starts"),
-        _buffer(lengths, _I32, index, (B,), "lengths"), _buffer(table, _I32, index, (B, width), "table"), width, B,
-        n if max_new is None else min(int(max_new), n), code, _raw_stream(index))
-    if status:
-        _check("baps_kv_append", status)
-
-
-@functools.lru_cache(maxsize=1024)
-def _attention_workspace(device: int, *sizes: int) -> int:
-    return int(load().baps_kv_attention_workspace(*sizes))
+    (_serving or _marshal()).append(cache, k_new, v_new, table, lengths, starts, max_new)
 
 
 def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int, page: int, table_width: int, window: Optional[int] = None,
                            sinks: int = 0) -> int:
     """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: none, or sizes that it refuses)."""
-    return _attention_workspace(_device(), B, H, Hkv, T, D, page, table_width, _window(window), int(sinks))
+    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D, page, table_width, min(int(_window(window)), ALL_KEYS), int(sinks)))
 
 
 def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int] = None, sinks: int = 0, scale: float = 0.0,
@@ -490,42 +416,7 @@ def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int
     strides), query t at position lengths[b]-T+t, T <= 16.  Returns out, or (out, lse float32 [B,H,T]) if ``want_lse``.
     ``workspace``: a uint8 tensor of ``kv_attention_workspace`` bytes, allocated here if not given; calls that may run at
     the same time need one each."""
-    code, index, shape = _dtype16(q, "q"), cache.here(), q.shape
-    B, H, T, D = shape
-    _, Hkv, page, Dc = cache.k.shape
-    rows, width = table.shape
-    window, sinks = _window(window), int(sinks)
-    if D != Dc or rows != B:
-        raise ValueError("q does not match the cache, or table is not [B,width]")
-    if out is None:
-        out = _empty_like(q)
-    if lse is not None:
-        lse_ptr = _buffer(lse, _F32, index, (B, H, T), "lse")
-    elif want_lse:
-        lse = cache.k_scale.new_empty((B, H, T))
-        lse_ptr = lse.data_ptr()
-    else:
-        lse_ptr = None
-    if workspace is None:
-        n = _attention_workspace(index, B, H, Hkv, T, D, page, width, window, sinks)
-        ws_ptr = (workspace := cache.k.new_empty((n,))).data_ptr() if n else None
-    elif workspace.dtype != _U8 or workspace.get_device() != index or not workspace.is_contiguous():
-        raise ValueError("workspace: expected a contiguous uint8 tensor on q's device")
-    else:
-        n, ws_ptr = workspace.numel(), workspace.data_ptr()
-    st = _pack("6q", *_stride3(q, q, shape, "q"), *_stride3(out, q, shape, "out"))
-    status = load().baps_kv_attention(
-        q.data_ptr(), out.data_ptr(), lse_ptr, cache.struct, _buffer(table, _I32, index, (B, width), "table"), width,
-        _buffer(lengths, _I32, index, (B,), "lengths"), st, B, H, T, window, sinks, float(scale), code, ws_ptr, n,
-        _raw_stream(index))
-    if status:
-        _check("baps_kv_attention", status)
-    return (out, lse) if want_lse else out
-
-
-@functools.lru_cache(maxsize=256)
-def _pages_workspace(rows: int, n_pages: int) -> int:
-    return int(load().baps_kv_pages_workspace(rows, n_pages))
+    return (_serving or _marshal()).attention(q, cache, table, lengths, _window(window), sinks, scale, out, want_lse, lse, workspace)
 
 
 def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int = 0, window: Optional[int] = None,
@@ -534,34 +425,9 @@ def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int 
     pages shared, last pages copied for all children of a parent but the first, pages outside the window let go, free pages
     (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a
     row that found no room has length -1."""
-    index = cache.here()
-    rows, width = table.shape
-    n_pages, (new_rows,) = cache.k.shape[0], parents.shape
-    ptrs = (_buffer(table, _I32, index, (rows, width), "table"), _buffer(lengths, _I32, index, (rows,), "lengths"),
-            _buffer(refs, _I32, index, (n_pages,), "refs"), _buffer(parents, _I32, index, (new_rows,), "parents"))
-    new = _empty_like(table) if new_rows == rows else table.new_empty((new_rows, width))
-    new_lengths, new_refs = _empty_like(parents), _empty_like(refs)
-    n = _pages_workspace(new_rows, n_pages)
-    ws = cache.k.new_empty((n,))
-    status = load().baps_kv_fork(cache.struct, ptrs[0], ptrs[1], rows, ptrs[2], ptrs[3], new_rows, width, int(reserve), _window(window),
-                                 int(sinks), new.data_ptr(), new_lengths.data_ptr(), new_refs.data_ptr(), ws.data_ptr(), n,
-                                 _raw_stream(index))
-    if status:
-        _check("baps_kv_fork", status)
-    return new, new_lengths, new_refs
+    return (_serving or _marshal()).fork(cache, table, lengths, refs, parents, reserve, _window(window), sinks)
 
 
 def baps_kv_compact(cache: KvCache, table, refs):
     """Move the pages in use to the front of the pool.  Returns (new_table, new_refs, page_map, n_live), all int32."""
-    index = cache.here()
-    rows, width = table.shape
-    n_pages = cache.k.shape[0]
-    table_ptr, refs_ptr = _buffer(table, _I32, index, (rows, width), "table"), _buffer(refs, _I32, index, (n_pages,), "refs")
-    new, new_refs, page_map, n_live = _empty_like(table), _empty_like(refs), _empty_like(refs), refs.new_empty((1,))
-    n = _pages_workspace(0, n_pages)
-    ws = cache.k.new_empty((n,))
-    status = load().baps_kv_compact(cache.struct, table_ptr, rows, width, refs_ptr, new.data_ptr(), new_refs.data_ptr(),
-                                    page_map.data_ptr(), n_live.data_ptr(), ws.data_ptr(), n, _raw_stream(index))
-    if status:
-        _check("baps_kv_compact", status)
-    return new, new_refs, page_map, n_live
+    return (_serving or _marshal()).compact(cache, table, refs)

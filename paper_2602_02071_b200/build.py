@@ -2,7 +2,8 @@
 
 Compiles the translation units of ``csrc/`` (``baps_lib.cu``: conversions, row softmax, BAPS attention; ``baps_serving.cu``:
 windowed attention, the 8-bit key-value cache and its pages) for sm_100a, side by side, and links them into
-``paper_2602_02071_b200/libbaps.so``.  nvcc cross-compiles, so no GPU is needed to build.
+``paper_2602_02071_b200/libbaps.so``.  nvcc cross-compiles, so no GPU is needed to build.  ``serving_marshal.c``, the binding's
+argument checks of the serving calls, becomes the extension module ``_serving.so``.
 """
 from __future__ import annotations
 
@@ -10,6 +11,7 @@ import os
 import re
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,6 +28,7 @@ NVCC_FLAGS = [
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",
 ]
 UNITS = ["baps_lib.cu", "baps_serving.cu"]
+MARSHAL = os.path.join(_HERE, "_serving.so")
 
 
 def _sources(path: str, seen=None):
@@ -79,8 +82,22 @@ def _compile(lib: str, extra_flags, log_name: str, force: bool, verbose: bool) -
     return lib
 
 
+def _compile_marshal(force: bool) -> None:
+    src = os.path.join(CSRC, "serving_marshal.c")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(p) for p in _sources(src)):
+        return
+    cmd = [os.environ.get("CC", "gcc"), "-std=c11", "-O2", "-Wall", "-Wextra", "-shared", "-fPIC",
+           "-I" + sysconfig.get_path("include"), "-o", MARSHAL + ".tmp", src]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(" ".join(cmd) + "\n" + res.stdout + res.stderr)
+        raise RuntimeError("the C compiler failed on serving_marshal.c")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library if it is missing or older than any source; return its path."""
+    """Compile the library and the binding's module if they are missing or older than any source; return the library's path."""
+    _compile_marshal(force)
     extra = os.environ.get("BAPS_NVCC_EXTRA", "").split()       # developer switch, e.g. -DNAME=1
     return _compile(LIB, extra, "build.log", force, verbose)
 
