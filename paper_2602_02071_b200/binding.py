@@ -346,7 +346,7 @@ def baps_attention_restart_rates_static(q, k, v, *, causal: bool, out: torch.Ten
 # ---- serving: windowed prompts, the 8-bit cache, its attention and its pages -----------------------------------------
 #
 # The smallest of these calls take a few microseconds on the device, less than the same checks take in Python.  So tensors are
-# checked, outputs allocated and pointers passed by an extension module built from csrc/serving_marshal.c, which calls the
+# checked, outputs allocated and pointers passed by an extension module built from csrc/serving_marshal.cpp, which calls the
 # functions of the library that load() returns.
 
 _serving = None
@@ -359,9 +359,7 @@ def _marshal():
     if _serving is None:
         from . import _serving as module
         lib = load()
-        module.bind((torch.bfloat16, torch.float16, torch.float32, torch.int32, torch.uint8, torch.empty_like, torch._C._cuda_getDevice,
-                     torch._C._cuda_getCurrentRawStream, _check),
-                    tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _SERVING_CALLS))
+        module.bind(_check, [ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _SERVING_CALLS])
         _serving = module
     return _serving
 
@@ -386,7 +384,7 @@ class KvCache:
     __slots__ = ("k", "v", "k_scale", "v_scale", "struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        self.struct = (_serving or _marshal()).cache_struct(k, v, k_scale, v_scale)          # baps_kv_cache
+        self.struct = (_serving or _marshal()).cache_struct(k, v, k_scale, v_scale)          # baps_kv_cache, device
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
 
     @classmethod

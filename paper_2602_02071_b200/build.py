@@ -2,13 +2,14 @@
 
 Compiles the translation units of ``csrc/`` (``baps_lib.cu``: conversions, row softmax, BAPS attention; ``baps_serving.cu``:
 windowed attention, the 8-bit key-value cache and its pages) for sm_100a, side by side, and links them into
-``paper_2602_02071_b200/libbaps.so``.  nvcc cross-compiles, so no GPU is needed to build.  ``serving_marshal.c``, the binding's
+``paper_2602_02071_b200/libbaps.so``.  nvcc cross-compiles, so no GPU is needed to build.  ``serving_marshal.cpp``, the binding's
 argument checks of the serving calls, becomes the extension module ``_serving.so``.
 """
 from __future__ import annotations
 
 import os
 import re
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -83,15 +84,20 @@ def _compile(lib: str, extra_flags, log_name: str, force: bool, verbose: bool) -
 
 
 def _compile_marshal(force: bool) -> None:
-    src = os.path.join(CSRC, "serving_marshal.c")
+    src = os.path.join(CSRC, "serving_marshal.cpp")
     if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(p) for p in _sources(src)):
         return
-    cmd = [os.environ.get("CC", "gcc"), "-std=c11", "-O2", "-Wall", "-Wextra", "-shared", "-fPIC",
-           "-I" + sysconfig.get_path("include"), "-o", MARSHAL + ".tmp", src]
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-Wextra", "-shared", "-fPIC",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_path("include"),
+           "-isystem", root + "/include", "-isystem", root + "/include/torch/csrc/api/include", "-isystem", cuda + "/include",
+           "-o", MARSHAL + ".tmp", src, "-L" + root + "/lib", "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(" ".join(cmd) + "\n" + res.stdout + res.stderr)
-        raise RuntimeError("the C compiler failed on serving_marshal.c")
+        raise RuntimeError("the C++ compiler failed on serving_marshal.cpp")
     os.replace(MARSHAL + ".tmp", MARSHAL)
 
 
