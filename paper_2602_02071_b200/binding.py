@@ -1,9 +1,9 @@
-"""Thin ctypes binding over the C ABI in ``include/baps.h``.
+"""Thin binding over the C ABI in ``include/baps.h``: ctypes, and for the serving calls the extension module ``_serving``.
 
 Argument marshalling only: every function takes torch CUDA tensors (used purely as device
 buffers), passes their pointers and the current CUDA stream to the entry point of the same
 name, and raises ``BapsError`` on a non-zero status.  Nothing here computes: if ``libbaps.so``
-is missing the import of the library fails loudly -- there is no fallback path.
+or ``_serving.so`` is missing the call fails loudly -- there is no fallback path.
 """
 from __future__ import annotations
 
