@@ -6,7 +6,8 @@
 // by a power of two per row so that its 8 or 11 bits fit fp16 (what is lost is below 2^-25 of the row's largest element),
 // and both products run on mma.sync m16n8k16 with float32 accumulation; the weights are rounded to fp16 (half a step, 2^-12)
 // after they have been summed.  The scales are applied in float32; O~ is kept in units of a value scale that is followed
-// where a page's leaves [unit / 64, unit].
+// where a page's leaves [unit / 64, unit], down to 2^-64 of the largest that there was: O~, below 2^14 * 448 in units of that one
+// for each key, then stays below 2^118 for 2^31 keys, and what is smaller does not count.
 //
 // What bounds it: the bytes of K and V, one per element: 48 sequences of 8192 to 32768 tokens, 32 / 8 heads of 128, pages of 64,
 // 298 us, 6.7 TB/s.  mma.sync, not tcgen05: the codes have to be widened in registers on the way, and a CTA has 8 to 32 rows of
@@ -395,6 +396,7 @@ kv_attention_kernel(const KvAttnParams p)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[qt][i][k] = 0.f;
         float unit = 0.f, inv_unit = 0.f;                                // value scale that O~ is in units of; 0: none yet
+        float unit_most = 0.f;                                           // the largest that it has been
         auto times = [&](int qt, float f0, float f1) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) { o[qt][i][0] *= f0; o[qt][i][1] *= f1; o[qt][i][2] *= f0; o[qt][i][3] *= f1; }
@@ -501,7 +503,8 @@ kv_attention_kernel(const KvAttnParams p)
                 const float v_most = fmaxf(va, vb), v_least = fminf(va, vb);
                 if (!(v_most <= unit && v_least * 64.f >= unit)) {
                     if (unit == 0.f) { unit = v_most; inv_unit = pow2_inverse(unit); }
-                    else if (v_most > unit * 5.421010862427522e-20f) to_unit(v_most);        // 2^-64; below, it does not count
+                    else if (v_most > unit_most * 5.421010862427522e-20f) to_unit(v_most);   // 2^-64; below, it does not count
+                    unit_most = fmaxf(unit_most, unit);
                 }
                 // ---- weights ---------------------------------------------------------------------------------------
 #pragma unroll
@@ -523,7 +526,7 @@ kv_attention_kernel(const KvAttnParams p)
                     float fa = va * inv_unit, fb = vb * inv_unit;        // powers of two up to 1
                     if (apart) {
                         const float mine = pass ? vb : va;
-                        if (mine > unit * 5.421010862427522e-20f && mine != unit) to_unit(mine);
+                        if (mine > unit_most * 5.421010862427522e-20f && mine != unit) to_unit(mine);
                         fa = pass ? 0.f : mine * inv_unit;
                         fb = pass ? mine * inv_unit : 0.f;
                     }
