@@ -1,6 +1,8 @@
 // Attention of the last T tokens of every sequence over the 8-bit cache.
 //
 //     s = c * k_scale * (q . k_code),  w = 2^(s - m),  l = sum w,  O~ = sum w * v_scale * v_code;   O = O~ / l
+// A part of the keys hands on its (m, l) and O, not O~: a sum of values may be beyond float32 where their mean is not.  Parts are
+// joined as  m = max m_i,  l = sum 2^(m_i - m) l_i,  O = sum (2^(m_i - m) l_i / l) O_i.
 // with c = log2(e) * scale and a running reference m, six below a maximum that is followed when a score passes it by more
 // than 8, so that weights stay below 2^14.  Codes become fp16 in registers (exactly: E4M3 has 4 significant bits), q is scaled
 // by a power of two per row so that its 8 or 11 bits fit fp16 (what is lost is below 2^-25 of the row's largest element),
@@ -48,7 +50,7 @@ struct KvAttnParams {
     int width, B, H, Hkv, T, G, R, groups;      // G = H / Hkv, R = T * G rows per kv head, in `groups` groups of kRows
     int n_pages, page, window, sinks;
     float c;
-    // workspace: per CTA two partial results (rows x (D floats)), (m, l) of their rows, and which item they belong to
+    // workspace: per CTA two partial results (rows x (D floats), divided by l), (m, l) of their rows, and which item they belong to
     float *part_o;
     float2 *part_ml;
     int2 *desc;                                  // (item, last CTA that has part of it); item -1: none begins here and goes on
@@ -56,6 +58,7 @@ struct KvAttnParams {
 
 constexpr int kKvTile = 64, kKvLogTile = 6, kKvStep = 32, kKvMaxB = 4096;
 constexpr int kKvMinTiles = 2;                   // tiles that a CTA takes at least
+constexpr int kKvMaxCluster = 8;                 // CTAs of a cluster at most
 
 // kTiles: groups of eight rows that a CTA serves.
 template <int D, int kTiles>
@@ -188,13 +191,13 @@ __device__ __forceinline__ void kv_store_lse(const KvAttnParams &p, int b, int h
 {
     if (p.lse) p.lse[((int64_t)b * p.H + h) * p.T + tq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
-// Elements d0 .. d0 + 3 of an output row from O~ and l (against the maximum m); d0 = 0 brings the lse along.
+__device__ __forceinline__ float kv_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }     // (0: no key at all)
+// Elements d0 .. d0 + 3 of an output row; d0 = 0 brings the lse along.
 template <typename T16>
 __device__ __forceinline__ void kv_store(const KvAttnParams &p, int b, int h, int tq, int d0, const float (&o)[4], float m, float l)
 {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2 *>(reinterpret_cast<T16 *>(p.out) + b * p.os_b + h * p.os_h + tq * p.os_t + d0) =
-        make_uint2(pack16<T16>(o[0] * inv, o[1] * inv), pack16<T16>(o[2] * inv, o[3] * inv));
+        make_uint2(pack16<T16>(o[0], o[1]), pack16<T16>(o[2], o[3]));
     if (d0 == 0) kv_store_lse(p, b, h, tq, m, l);
 }
 
@@ -569,18 +572,20 @@ kv_attention_kernel(const KvAttnParams p)
                 if (g == 0) ml[warp * 8 * kTiles + 8 * qt + 2 * t + e] = make_float2(m[qt][e], l[qt][e]);
             }
 #pragma unroll
-        for (int qt = 0; qt < kTiles; ++qt)
+        for (int qt = 0; qt < kTiles; ++qt) {
+            const float inv0 = kv_inverse(l[qt][0]), inv1 = kv_inverse(l[qt][1]);
 #pragma unroll
             for (int k = 0; k < D / 8; ++k)                              // element 8 k + g of rows 2 t, 2 t + 1
                 join[((warp * kTiles + qt) * (D / 8) + k) * 32 + lane] =
-                    make_float2(o[qt][k >> 1][2 * (k & 1)] * unit, o[qt][k >> 1][2 * (k & 1) + 1] * unit);
+                    make_float2(o[qt][k >> 1][2 * (k & 1)] * inv0 * unit, o[qt][k >> 1][2 * (k & 1) + 1] * inv1 * unit);
+        }
         __syncthreads();
         const bool whole = tiles == a.n;
         // Each warp joins every fourth of the (rows, 8 elements) entries, a thread what its own lane wrote: element 8 k + g of
         // rows 2 t, 2 t + 1 (no two lanes in a bank; read by output row, 16 at a time met in one and the join took 3700 cycles)
 #pragma unroll
         for (int qt = 0; qt < kTiles; ++qt) {
-            float M[2], Lsum[2], f[2][L::kWarps], inv[2];
+            float M[2], Lsum[2], f[2][L::kWarps];
             int64_t to[2];                                               // first element of the row, wherever it goes
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -593,14 +598,15 @@ kv_attention_kernel(const KvAttnParams p)
 #pragma unroll
                 for (int y = 0; y < L::kWarps; ++y) {
                     const float2 own = ml[y * 8 * kTiles + rr];
-                    f[e][y] = ex2_approx(own.x - Mu);
-                    Lsum[e] += f[e][y] * own.y;
+                    f[e][y] = ex2_approx(own.x - Mu) * own.y;
+                    Lsum[e] += f[e][y];
                 }
-                inv[e] = 1.f;
+                const float inv = kv_inverse(Lsum[e]);
+#pragma unroll
+                for (int y = 0; y < L::kWarps; ++y) f[e][y] *= inv;
                 if (kClusters) {
                     to[e] = rr * D;
                 } else if (whole) {
-                    inv[e] = Lsum[e] == 0.f ? 0.f : 1.f / Lsum[e];
                     to[e] = a.b * p.os_b + (hk * p.G + r / p.T) * p.os_h + r % p.T * p.os_t;
                 } else {
                     to[e] = ((int64_t)(2 * blockIdx.x + (a.i == 0 ? 1 : 0)) * L::kRows + rr) * D;
@@ -625,7 +631,7 @@ kv_attention_kernel(const KvAttnParams p)
                     if (to[e] < 0) continue;
                     const int64_t at = to[e] + 8 * k + g;
                     if (kClusters) reinterpret_cast<float *>(smem)[at] = acc[e];     // over the slots, which every warp is done with
-                    else if (whole) reinterpret_cast<T16 *>(p.out)[at] = from_float<T16>(acc[e] * inv[e]);
+                    else if (whole) reinterpret_cast<T16 *>(p.out)[at] = from_float<T16>(acc[e]);
                     else p.part_o[at] = acc[e];
                 }
             }
@@ -638,15 +644,24 @@ kv_attention_kernel(const KvAttnParams p)
                 if (r >= p.R) continue;
                 float M = -INFINITY, Lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
                 const uint32_t o_at = sbase + (uint32_t)((rr * D + d0) * 4), ml_at = sbase + (uint32_t)(L::kRows * D * 4 + rr * 8);
-                for (int y = 0; y < size; ++y) M = fmaxf(M, cluster_f32x2(cluster_addr(ml_at, y)).x);
+                float2 own[kKvMaxCluster];
+                float4 u[kKvMaxCluster];
+#pragma unroll
+                for (int y = 0; y < kKvMaxCluster; ++y) {                // (all on their way together)
+                    own[y] = make_float2(-INFINITY, 0.f);
+                    u[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (y < size) { own[y] = cluster_f32x2(cluster_addr(ml_at, y)); u[y] = cluster_f32x4(cluster_addr(o_at, y)); }
+                }
+#pragma unroll
+                for (int y = 0; y < kKvMaxCluster; ++y) M = fmaxf(M, own[y].x);
                 const float Mu = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-                for (int y = 0; y < size; ++y) {
-                    const float2 own = cluster_f32x2(cluster_addr(ml_at, y));
-                    const float4 u = cluster_f32x4(cluster_addr(o_at, y));
-                    const float f = ex2_approx(own.x - Mu);
-                    Lsum += f * own.y;
-                    acc[0] += f * u.x; acc[1] += f * u.y; acc[2] += f * u.z; acc[3] += f * u.w;
+#pragma unroll
+                for (int y = 0; y < kKvMaxCluster; ++y) Lsum += own[y].y *= ex2_approx(own[y].x - Mu);
+                const float inv = kv_inverse(Lsum);
+#pragma unroll
+                for (int y = 0; y < kKvMaxCluster; ++y) {
+                    const float f = own[y].y * inv;
+                    acc[0] += f * u[y].x; acc[1] += f * u[y].y; acc[2] += f * u[y].z; acc[3] += f * u[y].w;
                 }
                 kv_store<T16>(p, a.b, hk * p.G + r / p.T, r % p.T, d0, acc, M, Lsum);
             }
@@ -684,7 +699,7 @@ kv_join_kernel(const KvAttnParams p)
     const bool there = r < p.R;
     const int parts = what.y - (int)blockIdx.x + 1;
     auto row = [&](int k) { return (int64_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * kRows + rr; };
-    // each side its own parts against their own maximum, then the sides together
+    // each side its own parts against their own maximum, then the sides together; acc: O, l
     float m = -INFINITY, acc[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
     for (int k0 = 0; there && k0 < parts; k0 += kEach * kSide) {
         float4 u[kEach];
@@ -702,15 +717,20 @@ kv_join_kernel(const KvAttnParams p)
         float top = m;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) top = fmaxf(top, ml[i].x);
-        const float mu = top == -INFINITY ? 0.f : top, back = ex2_approx(m - mu);
+        const float mu = top == -INFINITY ? 0.f : top;
+        float back = ex2_approx(m - mu) * acc[4];
+        acc[4] = back;
 #pragma unroll
-        for (int e = 0; e < 5; ++e) acc[e] *= back;
+        for (int i = 0; i < kEach; ++i) acc[4] += ml[i].y *= ex2_approx(ml[i].x - mu);
+        const float inv = kv_inverse(acc[4]);
+        back *= inv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= back;
         m = top;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const float f = ex2_approx(ml[i].x - mu);
+            const float f = ml[i].y * inv;
             acc[0] += f * u[i].x; acc[1] += f * u[i].y; acc[2] += f * u[i].z; acc[3] += f * u[i].w;
-            acc[4] += f * ml[i].y;
         }
     }
 #pragma unroll
@@ -721,17 +741,17 @@ kv_join_kernel(const KvAttnParams p)
     float all = m;
 #pragma unroll
     for (int k = 1; k < kSide; ++k) all = fmaxf(all, s_o[sub][k][x][5]);
-    const float mu = all == -INFINITY ? 0.f : all, own = ex2_approx(m - mu);
+    const float mu = all == -INFINITY ? 0.f : all;
+    float f[kSide], l = 0.f;
 #pragma unroll
-    for (int e = 0; e < 5; ++e) acc[e] *= own;
+    for (int k = 0; k < kSide; ++k) l += f[k] = ex2_approx(s_o[sub][k][x][5] - mu) * s_o[sub][k][x][4];
+    const float inv = kv_inverse(l);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 1; k < kSide; ++k) {
-        const float f = ex2_approx(s_o[sub][k][x][5] - mu);
+    for (int k = 0; k < kSide; ++k)
 #pragma unroll
-        for (int e = 0; e < 5; ++e) acc[e] += f * s_o[sub][k][x][e];
-    }
-    const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
-    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, 4 * x, o, all, acc[4]);
+        for (int e = 0; e < 4; ++e) o[e] += f[k] * inv * s_o[sub][k][x][e];
+    kv_store<T16>(p, what.x / heads, hr / p.groups * p.G + r / p.T, r % p.T, 4 * x, o, all, l);
 }
 
 // Rows of a kv head go to a CTA 8 or 16 (D = 64: up to 32) at a time, as many as its registers hold; more are items of their own,
@@ -752,7 +772,7 @@ static inline KvShape kv_shape(int R, int D, int64_t items, int64_t most_tiles, 
     s.ctas = num_sms() * (D == 64 && s.tiles < 4 ? 3 : 2);
     s.cluster = 0;
     items *= s.groups;
-    for (int c = 1; c <= 8; ++c) {
+    for (int c = 1; c <= kKvMaxCluster; ++c) {
         const int64_t each = (most_tiles + c - 1) / c;
         const bool fits = items * c <= s.ctas, full = fits && 5 * items * c >= 4 * s.ctas;
         if (c == 1 ? each <= 24 : fits && (each <= 16 || (by_window && full && each <= 36))) s.cluster = c;

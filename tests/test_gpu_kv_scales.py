@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 # Exponents of the value scales of consecutive 128 keys (the keys that a CTA's four warps take at once, so that every warp meets
 # them one after the other).  2^-108 is what baps_kv_append gives a page of zeros.
-FALLS = [(60, 0, -60), (60, 0, -60, -108), (4, -48, -108), (0, 60, 0, -60), (-108, 0, -60, 60, 0, -60),
+FALLS = [(60, 0, -60), (60, 0, -60, -108), (4, -48, -108), (0, 60, 0, -60), (-108, 0, -60, 60, 0, -60), (110, 50, -10, -70),
          (-60, 0, 60, 0)]
 # B, H, Hkv, T, D, tokens, table room: a cluster of eight CTAs, a CTA per sequence and head, the even cut
 CUTS = [(1, 4, 1, 1, 64, 6144, 0), (80, 2, 2, 1, 64, 1536, 0), (80, 2, 2, 1, 64, 1536, 40000),
@@ -65,3 +65,23 @@ def test_falls_of_pages_that_the_append_has_scaled():
     state = [cache.k, cache.v, cache.k_scale, cache.v_scale]
     got = check(q, state, table.cpu(), torch.tensor([n], dtype=torch.int32), serving.NONE, 0)
     assert got.isfinite().all() and got.abs().min() > 1000
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("exponent", [100, 119])
+def test_values_at_the_end_of_float32(cut, exponent):
+    """Values of up to 448 * 2^119, the largest that baps_kv_append writes for bf16, and keys that all count: the sums over them are
+    beyond float32, their means are not."""
+    q, state, table, lengths = scaled(cut, 32, lambda j: exponent)
+    q = q * 2.0 ** -10
+    assert check(q, state, table, lengths, serving.NONE, 0).isfinite().all()
+    state[1].fill_(0x7E)                                           # 448 everywhere: the mean is the value
+    got = check(q, state, table, lengths, serving.NONE, 0)
+    assert ((got / (448 * 2.0 ** exponent) - 1).abs() <= 2.0 ** -8 + 2.0 ** -10).all()
+
+
+@pytest.mark.parametrize("cut", CUTS)
+def test_values_at_the_small_end(cut):
+    """Scales of 2^-108, the smallest that baps_kv_append writes."""
+    q, *rest = scaled(cut, 32, lambda j: -108)
+    assert check(q, *rest, serving.NONE, 0).abs().max() > 0
