@@ -379,13 +379,24 @@ def baps_attention_window_fwd(q, k, v, *, window: Optional[int], sinks: int = 0,
 
 
 class KvCache:
-    """A pool of pages of 8-bit keys and values: codes uint8 [n_pages,Hkv,page,D] (E4M3), scales float32 [n_pages,Hkv]."""
+    """A pool of pages of 8-bit keys and values: codes uint8 [n_pages,Hkv,page,D] (E4M3), scales float32 [n_pages,Hkv].
+
+    The members cannot be assigned: another pool is another ``KvCache``.  A call refuses a cache whose tensors no longer are
+    what they were when it was made (resized, or given other storage)."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        self.struct = (_serving or _marshal()).cache_struct(k, v, k_scale, v_scale)          # baps_kv_cache, device
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        (_serving or _marshal()).fill_cache(self, k, v, k_scale, v_scale)         # struct: bytes of a baps_kv_cache, device
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"KvCache.{name} cannot be assigned: make a new KvCache")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"KvCache.{name} cannot be deleted")
+
+    def __reduce__(self):                        # copies and pickles are made of their own tensors
+        return KvCache, (self.k, self.v, self.k_scale, self.v_scale)
 
     @classmethod
     def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":

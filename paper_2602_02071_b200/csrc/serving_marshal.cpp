@@ -28,6 +28,7 @@ namespace {
 
 PyObject* g_raise = nullptr;                       // binding._check(name, status)
 PyObject* g_struct = nullptr;                      // "struct"
+PyObject* g_members[4] = {};                       // "k", "v", "k_scale", "v_scale"
 struct Library {
     decltype(&baps_attention_window_fwd) window;
     decltype(&baps_kv_append) append;
@@ -140,6 +141,25 @@ struct Cache {
     baps_kv_cache c;
     int device;
 };
+// The struct of a KvCache's tensors.
+Cache cache_of_tensors(PyObject* const* a)
+{
+    const Tensor& k = tensor(a[0], "k");
+    const Sizes s = k.sizes();
+    if (s.size() != 4 || !k.is_cuda()) refuse("k", "CUDA codes [n_pages,Hkv,page,D]");
+    Cache cache;
+    std::memset(&cache, 0, sizeof(cache));         // padding too
+    cache.device = k.get_device();
+    cache.c.k = static_cast<decltype(cache.c.k)>(buffer(a[0], "k", kByte, s, cache.device));
+    cache.c.v = static_cast<decltype(cache.c.v)>(buffer(a[1], "v", kByte, s, cache.device));
+    cache.c.k_scale = static_cast<float*>(buffer(a[2], "k_scale", kFloat, s.slice(0, 2), cache.device));
+    cache.c.v_scale = static_cast<float*>(buffer(a[3], "v_scale", kFloat, s.slice(0, 2), cache.device));
+    cache.c.n_pages = size_of(s[0]);
+    cache.c.Hkv = size_of(s[1]);
+    cache.c.page = size_of(s[2]);
+    cache.c.D = size_of(s[3]);
+    return cache;
+}
 Cache cache_of(PyObject* o)
 {
     Cache cache;
@@ -149,6 +169,16 @@ Cache cache_of(PyObject* o)
     if (ok) std::memcpy(&cache, PyBytes_AS_STRING(bytes), sizeof(Cache));
     Py_DECREF(bytes);
     if (!ok) refuse("cache", "a KvCache");
+    // The struct's addresses are those of the tensors that the KvCache holds, or the memory may be another's by now.
+    struct Held {
+        PyObject* o[4] = {};
+        ~Held() { for (PyObject* x : o) Py_XDECREF(x); }
+    } held;
+    for (int i = 0; i < 4; ++i)
+        if (!(held.o[i] = PyObject_GetAttr(o, g_members[i]))) throw Raised();
+    const Cache now = cache_of_tensors(held.o);
+    if (std::memcmp(&now, &cache, sizeof(Cache)) != 0)
+        throw Refused{PyExc_ValueError, "cache: its tensors were resized or given other storage since the KvCache was made; make a new one"};
     is_current("the cache", cache.device);
     return cache;
 }
@@ -331,24 +361,17 @@ PyObject* call_compact(PyObject* const* a)
     return tuple(new_table, new_refs, page_map, n_live);
 }
 
-// (k, v, k_scale, v_scale) -> bytes of a Cache
-PyObject* cache_struct(PyObject* const* a)
+// (KvCache, k, v, k_scale, v_scale): its members, past its own refusal of assignments
+PyObject* fill_cache(PyObject* const* a)
 {
-    const Tensor& k = tensor(a[0], "k");
-    const Sizes s = k.sizes();
-    if (s.size() != 4 || !k.is_cuda()) refuse("k", "CUDA codes [n_pages,Hkv,page,D]");
-    Cache cache;
-    std::memset(&cache, 0, sizeof(cache));         // padding too
-    cache.device = k.get_device();
-    cache.c.k = static_cast<decltype(cache.c.k)>(buffer(a[0], "k", kByte, s, cache.device));
-    cache.c.v = static_cast<decltype(cache.c.v)>(buffer(a[1], "v", kByte, s, cache.device));
-    cache.c.k_scale = static_cast<float*>(buffer(a[2], "k_scale", kFloat, s.slice(0, 2), cache.device));
-    cache.c.v_scale = static_cast<float*>(buffer(a[3], "v_scale", kFloat, s.slice(0, 2), cache.device));
-    cache.c.n_pages = size_of(s[0]);
-    cache.c.Hkv = size_of(s[1]);
-    cache.c.page = size_of(s[2]);
-    cache.c.D = size_of(s[3]);
-    return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&cache), sizeof(cache));
+    const Cache cache = cache_of_tensors(a + 1);
+    PyObject* bytes = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&cache), sizeof(cache));
+    if (!bytes) throw Raised();
+    int failed = PyObject_GenericSetAttr(a[0], g_struct, bytes);
+    Py_DECREF(bytes);
+    for (int i = 0; !failed && i < 4; ++i) failed = PyObject_GenericSetAttr(a[0], g_members[i], a[1 + i]);
+    if (failed) throw Raised();
+    Py_RETURN_NONE;
 }
 
 // (binding._check, addresses of the library's functions in Library's order)
@@ -389,7 +412,7 @@ constexpr PyMethodDef method(const char* name)
 {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<kCall, kArgs>)), METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<bind, 2>("bind"),           method<cache_struct, 4>("cache_struct"), method<call_window, 9>("window"),
+PyMethodDef g_methods[] = {method<bind, 2>("bind"),           method<fill_cache, 5>("fill_cache"), method<call_window, 9>("window"),
                            method<call_append, 7>("append"),       method<call_attention, 11>("attention"),      method<call_fork, 8>("fork"),
                            method<call_compact, 3>("compact"),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", "Argument marshalling of the serving calls.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -398,6 +421,9 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", "Argument marshalling
 
 PyMODINIT_FUNC PyInit__serving()
 {
+    const char* const members[] = {"k", "v", "k_scale", "v_scale"};
+    for (int i = 0; i < 4; ++i)
+        if (!(g_members[i] = PyUnicode_InternFromString(members[i]))) return nullptr;
     g_struct = PyUnicode_InternFromString("struct");
     return g_struct ? PyModule_Create(&g_module) : nullptr;
 }

@@ -1,5 +1,7 @@
 """The extension module between binding.py and the serving entry points: what it refuses, hands back and holds on to."""
+import copy
 import gc
+import pickle
 import sys
 import threading
 
@@ -163,3 +165,63 @@ def test_threads_call_at_once_on_streams_of_their_own():
     for t in threads:
         t.join(timeout=60)
     assert not wrong and not any(t.is_alive() for t in threads)
+
+
+@pytest.mark.gpu
+def test_a_cache_whose_tensors_have_changed_is_refused():
+    """Calls go to the memory of the tensors that the KvCache holds, or nowhere."""
+    _, q, table, lengths, refs = made()
+    parents = torch.zeros(2, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    new = torch.ones(2, 2, 64, dtype=torch.float16, device="cuda")
+    changes = [lambda c: c.k.set_(torch.zeros_like(c.k)), lambda c: setattr(c.v, "data", torch.zeros_like(c.v)),
+               lambda c: c.k_scale.resize_(40, 2), lambda c: c.k.resize_(2, 2, 16, 64), lambda c: c.v.unsqueeze_(0),
+               lambda c: setattr(c.v_scale, "data", torch.ones(12, 2, device="cuda"))]
+    for change in changes:
+        cache = made()[0]
+        old = [t.detach() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]     # the memory of before, by other tensors
+        before = [t.clone() for t in old]
+        change(cache)
+        launches = binding.launch_count()
+        for call in (lambda: binding.baps_kv_attention(q, cache, table, lengths),
+                     lambda: binding.baps_kv_append(cache, new, new, table, lengths, starts),
+                     lambda: binding.baps_kv_fork(cache, table, lengths, refs, parents),
+                     lambda: binding.baps_kv_compact(cache, table, refs)):
+            with pytest.raises(ValueError):
+                call()
+        assert binding.launch_count() == launches
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(old, before))
+
+
+@pytest.mark.gpu
+def test_members_of_a_cache_cannot_be_assigned():
+    cache, q, table, lengths, _ = made()
+    held = {n: getattr(cache, n) for n in ("k", "v", "k_scale", "v_scale", "struct")}
+    for name, x in held.items():
+        with pytest.raises(AttributeError):
+            setattr(cache, name, x.clone() if name != "struct" else x)
+        with pytest.raises(AttributeError):
+            delattr(cache, name)
+        assert getattr(cache, name) is x
+    with pytest.raises(AttributeError):
+        cache.other = 1
+    binding.baps_kv_attention(q, cache, table, lengths)
+
+
+@pytest.mark.gpu
+def test_copies_of_a_cache_are_caches_of_their_own_tensors():
+    cache, q, table, lengths, _ = made()
+    want = binding.baps_kv_attention(q, cache, table, lengths)
+    loaded = pickle.loads(pickle.dumps(cache))
+    deep, shallow = copy.deepcopy(cache), copy.copy(cache)
+    assert shallow.k is cache.k and shallow.struct == cache.struct
+    starts = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    new = torch.ones(2, 2, 64, dtype=torch.float16, device="cuda")
+    before = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    for c in (loaded, deep):
+        assert c.k.data_ptr() != cache.k.data_ptr() and c.struct != cache.struct
+        assert torch.equal(binding.baps_kv_attention(q, c, table, lengths), want)
+        binding.baps_kv_append(c, new, new, table, lengths - 1, starts)
+        assert not torch.equal(c.k, before[0])
+    assert all(torch.equal(a, b) for a, b in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), before))
