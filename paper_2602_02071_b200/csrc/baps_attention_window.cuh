@@ -36,6 +36,7 @@
 #include "baps_register_split.cuh"
 #include "baps_sm100.cuh"
 #include "baps_tma_host.cuh"
+#include "baps_visible.cuh"
 
 namespace baps {
 
@@ -49,7 +50,7 @@ struct WindowParams {
     float *lse;
     const int32_t *lengths;
     int64_t os_b, os_h, os_s;      // strides of out, elements
-    int B, H, Hkv, S, window, sinks, nitems;          // nitems: work items per head, of one or two query tiles
+    int B, H, Hkv, S, window, sinks, nitems;          // window: up to S; nitems: work items per head, of one or two query tiles
     float c;
 };
 
@@ -73,25 +74,6 @@ struct WinLayout {
     static constexpr int kDynBytes = kMiscOff + 16 + 1024;
     static_assert((D == 128 && kKeys == 128) || (D == 64 && kKeys == 64 && kStreams == 1), "forms that are looked after");
 };
-
-// Key tiles that rows [r0, r1] see (r0 <= r1): first tokens' tiles 0 .. ns - 1, then w0 .. w1.
-struct KeyTiles {
-    int ns, w0, w1;
-    __host__ __device__ int count() const { return ns + w1 - w0 + 1; }
-    __host__ __device__ int tile(int i) const { return i < ns ? i : w0 + i - ns; }
-    __host__ __device__ bool has(int tile) const { return tile < ns || (tile >= w0 && tile <= w1); }
-};
-__host__ __device__ inline KeyTiles key_tiles(int r0, int r1, int window, int sinks, int log2_tile)
-{
-    const int lo = r0 - window >= 0 ? r0 - window + 1 : 0;          // (no overflow: r0 >= 0, window >= 1)
-    KeyTiles k;
-    k.w0 = lo >> log2_tile;
-    k.w1 = r1 >> log2_tile;
-    const int seen = sinks < lo ? sinks : lo;                       // first tokens left of the window
-    k.ns = seen > 0 ? ((seen - 1) >> log2_tile) + 1 : 0;
-    if (k.ns > k.w0) k.ns = k.w0;
-    return k;
-}
 
 template <typename T16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi)
@@ -318,12 +300,8 @@ window_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             tmem_wait_ld();
             bool no_x = false, no_y = false;              // no row of the warp sees any key of the chunk
             if (!all) {
-                // columns b0 .. b0 + 31 that the row sees, as bits
-                auto visible = [&](int b0) -> uint32_t {
-                    auto below = [&](int v) -> uint32_t { v -= b0; return v <= 0 ? 0u : v >= 32 ? 0xffffffffu : (1u << v) - 1u; };
-                    return (below(r + 1) & ~below(r - p.window + 1)) | (below(p.sinks) & below(r + 1));
-                };
-                const uint32_t sx = visible(c0 + ch * 64), sy = visible(c0 + ch * 64 + 32);
+                const uint32_t sx = visible_columns(r, c0 + ch * 64, p.window, p.sinks);
+                const uint32_t sy = visible_columns(r, c0 + ch * 64 + 32, p.window, p.sinks);
                 no_x = !__any_sync(0xffffffffu, sx != 0u);
                 no_y = !__any_sync(0xffffffffu, sy != 0u);
                 if (!no_x && !__all_sync(0xffffffffu, sx == 0xffffffffu)) {

@@ -48,7 +48,7 @@ struct KvAttnParams {
     const uint8_t *k, *v;
     const float *k_scale, *v_scale;
     int width, B, H, Hkv, T, G, R, groups;      // G = H / Hkv, R = T * G rows per kv head, in `groups` groups of kRows
-    int n_pages, page, window, sinks;
+    int n_pages, page, window, sinks;           // window: up to width * page
     float c;
     // workspace: per CTA two partial results (rows x (D floats), divided by l), (m, l) of their rows, and which item they belong to
     float *part_o;
@@ -461,7 +461,7 @@ kv_attention_kernel(const KvAttnParams p)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const int j = c0 + 16 * blk + s_key[k >> 1], at_pos = pos[qt][k & 1];
-                                if (gone || !(j <= at_pos && (j > at_pos - p.window || j < p.sinks))) sc[qt][blk][k] = -INFINITY;
+                                if (gone || !sees(at_pos, j, p.window, p.sinks)) sc[qt][blk][k] = -INFINITY;
                             }
                         keep[blk] = 0u;
 #pragma unroll

@@ -68,7 +68,7 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
     if (B <= 0 || H <= 0 || Hkv <= 0 || S <= 0 || D <= 0 || H % Hkv != 0) return BAPS_ERR_INVALID_ARG;
     const baps_status st = check_softmax(window, sinks, scale, dtype);
     if (st != BAPS_OK) return st;
-    if ((D != 64 && D != 128) || B > 65535 || H > 65535 || S > 0x7fffff00) return BAPS_ERR_UNSUPPORTED;
+    if ((D != 64 && D != 128) || B > 65535 || H > 65535 || S > kMostPlaces) return BAPS_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(lse) || !aligned4(lengths)) return BAPS_ERR_ALIGNMENT;
     int64_t s[12];
     for (int i = 0; i < 4; ++i) {
@@ -88,7 +88,7 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
     WindowParams p;
     p.out = out; p.lse = lse; p.lengths = lengths;
     p.os_b = s[9]; p.os_h = s[10]; p.os_s = s[11];
-    p.B = B; p.H = H; p.Hkv = Hkv; p.S = S; p.window = window; p.sinks = sinks;
+    p.B = B; p.H = H; p.Hkv = Hkv; p.S = S; p.window = limited_window(window, S); p.sinks = sinks;
     p.c = base2_scale(scale, D);
     return half ? window_shape<__half>(maps, p, D, as_stream(stream)) : window_shape<__nv_bfloat16>(maps, p, D, as_stream(stream));
 }
@@ -166,7 +166,7 @@ baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_k
     p.qs_b = s[0]; p.qs_h = s[1]; p.qs_t = s[2]; p.os_b = s[3]; p.os_h = s[4]; p.os_t = s[5];
     p.table = table; p.lengths = lengths; p.k = cache->k; p.v = cache->v; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
     p.width = table_width; p.B = B; p.H = H; p.Hkv = cache->Hkv; p.T = T; p.G = H / cache->Hkv; p.R = T * p.G; p.groups = shape.groups;
-    p.n_pages = cache->n_pages; p.page = cache->page; p.window = window; p.sinks = sinks;
+    p.n_pages = cache->n_pages; p.page = cache->page; p.window = limited_window(window, places); p.sinks = sinks;
     p.c = base2_scale(scale, D);
     const size_t part_rows = (size_t)shape.ctas * 2 * 8 * shape.tiles;
     p.part_o = static_cast<float *>(workspace);
