@@ -296,7 +296,7 @@ size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page
  *     first row that finds too few, and every row behind it, gets length -1 and no pages; so does a row that
  *     table_width cannot hold (which takes none from the rows behind it).
  *   - new_refs[p]: number of entries of new_table that name page p.  new_table is -1 elsewhere.
- * refs, new_refs: device int32 [cache->n_pages]; table [rows, table_width], new_table [new_rows, table_width]; lengths [rows],
+ * refs (16-byte aligned, the other arrays 4-byte), new_refs: device int32 [cache->n_pages]; table [rows, table_width], new_table [new_rows, table_width]; lengths [rows],
  * new_lengths [new_rows].  In- and outputs must not overlap.  workspace: at least baps_kv_pages_workspace(new_rows, n_pages)
  * bytes.  cache->k and v are only written for copies.                                                      */
 baps_status baps_kv_fork(const baps_kv_cache *cache, const int32_t *table, const int32_t *lengths, int rows,

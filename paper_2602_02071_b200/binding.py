@@ -432,7 +432,7 @@ def baps_kv_fork(cache: KvCache, table, lengths, refs, parents, *, reserve: int 
                  sinks: int = 0):
     """Rebuild the rows of a batch: new row i continues old row parents[i] (outside the table: an empty row), full
     pages shared, last pages copied for all children of a parent but the first, pages outside the window let go, free pages
-    (refs == 0, lowest first) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a
+    (refs == 0, lowest first; ``refs`` 16-byte aligned) behind for ``reserve`` more tokens.  Returns (new_table, new_lengths, new_refs), all int32; a
     row that found no room has length -1."""
     return (_serving or _marshal()).fork(cache, table, lengths, refs, parents, reserve, _window(window), sinks)
 

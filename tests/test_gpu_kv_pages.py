@@ -179,3 +179,24 @@ def test_refusals():
         binding.baps_kv_compact(cache, t, r.float())
     with pytest.raises(ValueError):
         binding.baps_kv_compact(cache, t[:, ::2], r)
+
+
+def test_counts_that_are_a_slice_of_a_larger_array():
+    """refs is read 16 bytes at a time: a slice that begins on a multiple of four is taken, any other refused."""
+    page, n_pages = 16, 9
+    table, lengths, refs = [[0, 3]], [20], [1, 0, 0, 1, 0, 1, 0, 0, 0]
+    state = pool(n_pages, 1, page, 64, 1)
+    cache, parents = binding.KvCache(*state), ints([0, 0])
+    want = serving.fork(table, lengths, refs, [0, 0], page, n_pages, 0, serving.NONE, 0)
+    for at in range(6):
+        part = ints([7] * at + refs + [7] * 5)[at:at + n_pages]
+        if at % 4 == 0:
+            got = binding.baps_kv_fork(cache, ints(table), ints(lengths), part, parents)
+            assert [g.tolist() for g in got] == list(want[:3])
+        else:
+            n = binding.launch_count()
+            with pytest.raises(binding.BapsError) as e:
+                binding.baps_kv_fork(cache, ints(table), ints(lengths), part, parents)
+            assert e.value.status == -3 and binding.launch_count() == n
+        got = binding.baps_kv_compact(cache, ints(table), part)              # any alignment
+        assert got[1].tolist() == serving.compact(table, refs)[1]
