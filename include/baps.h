@@ -229,7 +229,8 @@ baps_status baps_attention_restart_rates_static(const void *q, const void *k, co
  * strides: NULL for contiguous [B, heads, S, D], else 12 int64 in elements: batch, head and row of q, k, v and out,
  * each at least 8 and a multiple of 8; the D elements of a row are contiguous.  Tensors must not overlap out.
  * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q, k, v and out).  scale: 0 selects 1/sqrt(D).
- * Supported (else BAPS_ERR_UNSUPPORTED): D in {64, 128}; any S >= 1; H % Hkv == 0; B, H <= 65535.           */
+ * Supported (else BAPS_ERR_UNSUPPORTED): D in {64, 128}; 1 <= S <= 2^31 - 256; H % Hkv == 0; B, H <= 65535;
+ * B * H * (query tiles of 128 rows) < 2^31.                                                                */
 baps_status baps_attention_window_fwd(const void *q, const void *k, const void *v, void *out, float *lse,
                                       const int32_t *lengths, const int64_t *strides, int B, int H, int Hkv, int S,
                                       int D, int window, int sinks, float scale, int dtype, baps_stream stream);
@@ -237,7 +238,8 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
 /* ---- The cache ---------------------------------------------------------------------------------------
  * A pool of pages.  k, v: [n_pages, Hkv, page, D] FP8 E4M3 codes (OCP, as in baps_attention_fwd_fp8); k_scale, v_scale:
  * [n_pages, Hkv] float32, one power of two per page and head: an element stands for value(code) * scale.  All device memory of
- * the caller, codes 16-byte and scales 4-byte aligned.  page in {16, 32, 64, 128}, D in {64, 128}.
+ * the caller, codes 16-byte and scales 4-byte aligned.  Supported by every call (else BAPS_ERR_UNSUPPORTED): page in
+ * {16, 32, 64, 128}, D in {64, 128}, Hkv <= 32767, n_pages * Hkv * page < 2^31.
  * A sequence's pages are named by its row of a table, int32 [rows, table_width]: token j stands at place j % page of page
  * table[row][j / page].  An entry outside 0 .. n_pages - 1 (-1 by convention) names no page: nothing is written there,
  * and its keys are invisible.                                                                          */
@@ -260,7 +262,7 @@ typedef struct {
  * nearest even, infinities to +-448, NaN to NaN.  A page whose first place is written begins anew.
  * Two sequences must not write to one page in the same call.  Codes and scales do not depend on how tokens are spread
  * over calls, but for the second rounding of elements that a grown scale makes subnormal.
- * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16.                                                             */
+ * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16.  Supported: B <= 65535; 2 * Hkv * (pages that max_new tokens touch) < 2^31.  */
 baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const void *v_new, const int64_t *strides,
                            int64_t n_tokens, const int32_t *starts, const int32_t *lengths, const int32_t *table,
                            int table_width, int B, int max_new, int dtype, baps_stream stream);
@@ -275,7 +277,9 @@ baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const 
  * irrelevant before and after; calls that may run at the same time need one each.
  * Value scales of a sequence and head that are more than 2^64 apart: the smaller values may count as zero.
  * Results are the same from call to call.  dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q and out).  scale: 0: 1/sqrt(D).
- * Supported: T <= 16; H % Hkv == 0; B <= 4096.                                                             */
+ * Supported (else BAPS_ERR_UNSUPPORTED): T <= 16; H % Hkv == 0; T * H / Hkv <= 65536; B <= 4096; table_width * page < 2^31 - 64;
+ * and fewer than 2^31 - 4096 key tiles in all: 64-key tiles of a table row, or of window + sinks if those are fewer, times
+ * B * Hkv * (groups of T * H / Hkv rows: 8 to 32 a group).                                                    */
 baps_status baps_kv_attention(const void *q, void *out, float *lse, const baps_kv_cache *cache, const int32_t *table,
                               int table_width, const int32_t *lengths, const int64_t *strides, int B, int H, int T,
                               int window, int sinks, float scale, int dtype, void *workspace, size_t workspace_bytes,
@@ -298,7 +302,8 @@ size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page
  *   - new_refs[p]: number of entries of new_table that name page p.  new_table is -1 elsewhere.
  * refs (16-byte aligned, the other arrays 4-byte), new_refs: device int32 [cache->n_pages]; table [rows, table_width], new_table [new_rows, table_width]; lengths [rows],
  * new_lengths [new_rows].  In- and outputs must not overlap.  workspace: at least baps_kv_pages_workspace(new_rows, n_pages)
- * bytes.  cache->k and v are only written for copies.                                                      */
+ * bytes, 16-byte aligned.  cache->k and v are only written for copies.
+ * Supported (else BAPS_ERR_UNSUPPORTED): rows <= 8192; new_rows * (table_width + 1) < 2^31.                    */
 baps_status baps_kv_fork(const baps_kv_cache *cache, const int32_t *table, const int32_t *lengths, int rows,
                          const int32_t *refs, const int32_t *parents, int new_rows, int table_width, int reserve,
                          int window, int sinks, int32_t *new_table, int32_t *new_lengths, int32_t *new_refs,
@@ -309,7 +314,8 @@ baps_status baps_kv_fork(const baps_kv_cache *cache, const int32_t *table, const
  * before n: codes, scales and count; all others stay.  page_map[p]: where page p is now (-1: free);
  * new_table = page_map of table (-1 stays); new_refs: the counts at their new places, 0 from n on.
  * Device int32 arrays: table, new_table [rows, table_width] (rows may be 0), refs, new_refs, page_map [n_pages],
- * n_live [1].  In- and outputs must not overlap.                                                          */
+ * n_live [1].  In- and outputs must not overlap.  workspace: at least baps_kv_pages_workspace(0, n_pages) bytes, 16-byte
+ * aligned.                                                                                                  */
 baps_status baps_kv_compact(const baps_kv_cache *cache, const int32_t *table, int rows, int table_width, const int32_t *refs,
                             int32_t *new_table, int32_t *new_refs, int32_t *page_map, int32_t *n_live,
                             void *workspace, size_t workspace_bytes, baps_stream stream);

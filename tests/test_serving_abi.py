@@ -114,3 +114,17 @@ def test_workspaces(lib):
     assert attention(lib, width=10000, window=1 << 30, ws=None) == attention(lib, width=10000, window=1 << 30, ws_bytes=1000) == -1
     pages = lib.baps_kv_pages_workspace
     assert pages(0, 1) > 0 and pages(10, 1000) > pages(0, 1000) and pages(-1, 5) == pages(3, 0) == 0
+
+
+def test_limits_of_sizes_that_the_header_names(lib):
+    """Sizes just beyond each limit; nothing is read or launched for them."""
+    for c in (cache(Hkv=32768), cache(n_pages=1 << 26, Hkv=2, page=16), cache(n_pages=1 << 20, Hkv=16, page=128)):
+        for call in (append, attention, fork, compact):
+            assert call(lib, c=c) == -2
+    assert window(lib, S=2 ** 31 - 255) == window(lib, B=65536) == window(lib, H=65536) == -2
+    assert append(lib, B=65536) == -2
+    for bad in (dict(T=16, H=2 * 4097), dict(B=4097), dict(T=17), dict(width=(2 ** 31 - 64) // 16),
+                dict(B=4096, width=1 << 20, window=2 ** 31 - 1)):
+        assert attention(lib, **bad) == -2, bad
+    assert fork(lib, rows=8193) == fork(lib, new_rows=1 << 20, width=(1 << 11) - 1) == -2
+    assert compact(lib, ws=BAD) == fork(lib, ws=BAD) == -3
