@@ -44,18 +44,31 @@ def _sources(path: str, seen=None):
     return seen
 
 
+def _portable(cmd) -> str:
+    """A command as one line that is the same wherever the tree stands."""
+    return " ".join(cmd).replace(os.path.normpath(os.path.join(_HERE, "..")) + os.sep, "")
+
+
+def _is_current(path: str, log: str, line: str, sources) -> bool:
+    """Whether ``path`` is there, no older than its sources, and made by this command (the first line of its log)."""
+    if not (os.path.exists(path) and os.path.exists(log)) or os.path.getmtime(path) < max(os.path.getmtime(p) for p in sources):
+        return False
+    with open(log) as f:
+        return f.readline() == line + "\n"
+
+
 def _compile_unit(unit: str, lib: str, extra_flags, force: bool):
-    """One object file next to the library, if it is missing or older than a source; returns (path, compiler's output)."""
+    """One object file next to the library, if it is missing, older than a source or made by another command; returns
+    (path, compiler's output)."""
     obj = f"{lib}.{os.path.splitext(unit)[0]}.o"
     src = os.path.join(CSRC, unit)
     log = obj + ".log"
-    if not force and os.path.exists(obj) and os.path.exists(log) and \
-            os.path.getmtime(obj) >= max(os.path.getmtime(p) for p in _sources(src)):
+    cmd = [os.environ.get("NVCC", "nvcc"), *NVCC_FLAGS, *extra_flags, "-c", "-o", obj + ".tmp", src]
+    if not force and _is_current(obj, log, _portable(cmd), _sources(src)):
         with open(log) as f:
             return obj, f.read()
-    cmd = [os.environ.get("NVCC", "nvcc"), *NVCC_FLAGS, *extra_flags, "-c", "-o", obj + ".tmp", src]
     res = subprocess.run(cmd, capture_output=True, text=True)
-    text = " ".join(cmd) + "\n" + res.stdout + res.stderr
+    text = _portable(cmd) + "\n" + res.stdout + res.stderr
     if res.returncode != 0:
         sys.stderr.write(text)
         raise RuntimeError(f"nvcc failed on {unit}")
@@ -66,16 +79,17 @@ def _compile_unit(unit: str, lib: str, extra_flags, force: bool):
 
 
 def _compile(lib: str, extra_flags, log_name: str, force: bool, verbose: bool) -> str:
-    newest = max(os.path.getmtime(p) for u in UNITS for p in _sources(os.path.join(CSRC, u)))
-    if not force and os.path.exists(lib) and os.path.getmtime(lib) >= newest:
+    key = _portable([os.environ.get("NVCC", "nvcc"), *NVCC_FLAGS, *extra_flags, *UNITS])
+    path = os.path.join(_HERE, log_name)
+    if not force and _is_current(lib, path, key, {p for u in UNITS for p in _sources(os.path.join(CSRC, u))}):
         return lib
     with ThreadPoolExecutor(len(UNITS)) as pool:
         done = list(pool.map(lambda u: _compile_unit(u, lib, extra_flags, force), UNITS))
     cmd = [os.environ.get("NVCC", "nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "--shared", "-o", lib, *(o for o, _ in done)]
     res = subprocess.run(cmd, capture_output=True, text=True)
-    log = "".join(t for _, t in done) + " ".join(cmd) + "\n" + res.stdout + res.stderr
-    with open(os.path.join(_HERE, log_name), "w") as f:
-        f.write(log)
+    log = "".join(t for _, t in done) + _portable(cmd) + "\n" + res.stdout + res.stderr
+    with open(path, "w") as f:
+        f.write((key if res.returncode == 0 else "failed") + "\n" + log)
     if verbose or res.returncode != 0:
         sys.stderr.write(log)
     if res.returncode != 0:
@@ -85,8 +99,6 @@ def _compile(lib: str, extra_flags, log_name: str, force: bool, verbose: bool) -
 
 def _compile_marshal(force: bool) -> None:
     src = os.path.join(CSRC, "serving_marshal.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(p) for p in _sources(src)):
-        return
     import torch
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))
@@ -94,15 +106,22 @@ def _compile_marshal(force: bool) -> None:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_path("include"),
            "-isystem", root + "/include", "-isystem", root + "/include/torch/csrc/api/include", "-isystem", cuda + "/include",
            "-o", MARSHAL + ".tmp", src, "-L" + root + "/lib", "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    # (compiled against the C++ interfaces of this torch and this Python)
+    key, log = f"torch {torch.__version__}, Python {sys.version.split()[0]}: " + _portable(cmd), MARSHAL + ".o.log"
+    if not force and _is_current(MARSHAL, log, key, _sources(src)):
+        return
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(" ".join(cmd) + "\n" + res.stdout + res.stderr)
         raise RuntimeError("the C++ compiler failed on serving_marshal.cpp")
+    with open(log, "w") as f:
+        f.write(key + "\n" + res.stdout + res.stderr)
     os.replace(MARSHAL + ".tmp", MARSHAL)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library and the binding's module if they are missing or older than any source; return the library's path."""
+    """Compile the library and the binding's module if they are missing, older than any source or made by another command (other
+    flags, another compiler, torch or Python); return the library's path."""
     _compile_marshal(force)
     extra = os.environ.get("BAPS_NVCC_EXTRA", "").split()       # developer switch, e.g. -DNAME=1
     return _compile(LIB, extra, "build.log", force, verbose)
