@@ -27,6 +27,8 @@ WAIT_TEST_FLAGS = ["-DBAPS_WAIT_LIMIT_NS=1000000ull", "-DBAPS_TEST_SKIP_LOAD=1"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",
+    # inline variables (the count of launches, the lock of the set-up) belong to one library, also where a process loads two builds
+    "-Xcompiler", "-fno-gnu-unique",
 ]
 UNITS = ["baps_lib.cu", "baps_serving.cu"]
 MARSHAL = os.path.join(_HERE, "_serving.so")
