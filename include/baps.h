@@ -228,7 +228,7 @@ baps_status baps_attention_restart_rates_static(const void *q, const void *k, co
  * q, k and v does not matter.  lse: NULL or device float [B, H, S], the natural logarithm of the sum of exponentials.
  * strides: NULL for contiguous [B, heads, S, D], else 12 int64 in elements: batch, head and row of q, k, v and out,
  * each at least 8 and a multiple of 8; the D elements of a row are contiguous.  Tensors must not overlap out.
- * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q, k, v and out).  scale: 0 selects 1/sqrt(D).
+ * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q, k, v and out).  scale: 0 selects 1/sqrt(D), at most 2^127.
  * Supported (else BAPS_ERR_UNSUPPORTED): D in {64, 128}; 1 <= S <= 2^31 - 256; H % Hkv == 0; B, H <= 65535;
  * B * H * (query tiles of 128 rows) < 2^31.                                                                */
 baps_status baps_attention_window_fwd(const void *q, const void *k, const void *v, void *out, float *lse,
@@ -276,7 +276,7 @@ baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const 
  * workspace: device memory, 16-byte aligned, at least baps_kv_attention_workspace() bytes (NULL if those are 0), contents
  * irrelevant before and after; calls that may run at the same time need one each.
  * Value scales of a sequence and head that are more than 2^64 apart: the smaller values may count as zero.
- * Results are the same from call to call.  dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q and out).  scale: 0: 1/sqrt(D).
+ * Results are the same from call to call.  dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q and out).  scale: as above.
  * Supported (else BAPS_ERR_UNSUPPORTED): T <= 16; H % Hkv == 0; T * H / Hkv <= 65536; B <= 4096; table_width * page < 2^31 - 64;
  * and fewer than 2^31 - 4096 key tiles in all: 64-key tiles of a table row, or of window + sinks if those are fewer, times
  * B * Hkv * (groups of T * H / Hkv rows: 8 to 32 a group).                                                    */

@@ -19,13 +19,15 @@ bool strides_ok(const int64_t *s, int n)
     return true;
 }
 
+float base2_scale(float scale, int D) { return (float)(1.4426950408889634074 * (scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)D))); }
+
 // Visibility, scale and type, shared by the two attention calls.
 baps_status check_softmax(int window, int sinks, float scale, int dtype)
 {
-    if (window < 1 || sinks < 0 || !(scale >= 0.f) || !std::isfinite(scale)) return BAPS_ERR_INVALID_ARG;
+    // (a scale that is infinite in base 2 makes NaN of a score of 0)
+    if (window < 1 || sinks < 0 || !(scale >= 0.f) || !std::isfinite(base2_scale(scale, 64))) return BAPS_ERR_INVALID_ARG;
     return dtype == BAPS_DTYPE_BF16 || dtype == BAPS_DTYPE_F16 ? BAPS_OK : BAPS_ERR_UNSUPPORTED;
 }
-float base2_scale(float scale, int D) { return (float)(1.4426950408889634074 * (scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)D))); }
 
 baps_status check_cache(const baps_kv_cache *c)
 {

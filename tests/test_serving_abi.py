@@ -128,3 +128,9 @@ def test_limits_of_sizes_that_the_header_names(lib):
         assert attention(lib, **bad) == -2, bad
     assert fork(lib, rows=8193) == fork(lib, new_rows=1 << 20, width=(1 << 11) - 1) == -2
     assert compact(lib, ws=BAD) == fork(lib, ws=BAD) == -3
+
+
+def test_a_scale_that_is_infinite_in_base_2_is_refused(lib):
+    for call in (window, attention):
+        assert call(lib, scale=3.4e38) == call(lib, scale=2.4e38) == call(lib, scale=float("inf")) == -1
+        assert call(lib, scale=2.0 ** 127, dtype=binding.DTYPE_F32) == -2              # taken: the type is what is refused
