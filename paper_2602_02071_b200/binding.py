@@ -415,7 +415,10 @@ def baps_kv_append(cache: KvCache, k_new, v_new, table, lengths, starts, *, max_
 def kv_attention_workspace(B: int, H: int, Hkv: int, T: int, D: int, page: int, table_width: int, window: Optional[int] = None,
                            sinks: int = 0) -> int:
     """Bytes of workspace that ``baps_kv_attention`` needs for these sizes (0: none, or sizes that it refuses)."""
-    return int(load().baps_kv_attention_workspace(B, H, Hkv, T, D, page, table_width, min(int(_window(window)), ALL_KEYS), int(sinks)))
+    sizes = [int(x) for x in (B, H, Hkv, T, D, page, table_width, min(_window(window), ALL_KEYS), sinks)]
+    if not all(0 <= x <= ALL_KEYS for x in sizes):                # (ctypes would keep the lower 32 bits)
+        return 0
+    return int(load().baps_kv_attention_workspace(*sizes))
 
 
 def baps_kv_attention(q, cache: KvCache, table, lengths, *, window: Optional[int] = None, sinks: int = 0, scale: float = 0.0,

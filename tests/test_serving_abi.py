@@ -134,3 +134,12 @@ def test_a_scale_that_is_infinite_in_base_2_is_refused(lib):
     for call in (window, attention):
         assert call(lib, scale=3.4e38) == call(lib, scale=2.4e38) == call(lib, scale=float("inf")) == -1
         assert call(lib, scale=2.0 ** 127, dtype=binding.DTYPE_F32) == -2              # taken: the type is what is refused
+
+
+def test_sizes_beyond_an_int_need_no_workspace(lib):
+    sizes = dict(B=1, H=8, Hkv=8, T=1, D=64, page=16, table_width=10000, window=None, sinks=0)
+    assert binding.kv_attention_workspace(**sizes) == binding.kv_attention_workspace(**{**sizes, "window": 2 ** 40}) > 0
+    for name in ("B", "H", "Hkv", "T", "D", "page", "table_width", "sinks"):
+        for far in (2 ** 32, -2 ** 32):
+            assert binding.kv_attention_workspace(**{**sizes, name: sizes[name] + far}) == 0, name
+    assert binding.kv_attention_workspace(**{**sizes, "window": -2 ** 32 + 5}) == 0
