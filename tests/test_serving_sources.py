@@ -60,3 +60,44 @@ def test_the_windowed_kernel_has_the_registers_that_its_roles_share_out():
     used = re.findall(r"Compiling entry function '\w*window_attention_kernelI\w*Li128ELi2ELi128E\w*'.*?Used (\d+) registers", log, re.S)
     # 128 threads at 64 and 512 at 104 out of 640 at what the kernel was compiled to
     assert len(used) == 2 and all(128 * 64 + 512 * 104 <= 640 * int(r) for r in used)
+
+
+def block_end(code, at):
+    """Index behind the brace that closes the one at or behind ``at``."""
+    depth, i = 0, code.index("{", at)
+    while True:
+        depth += {"{": 1, "}": -1}.get(code[i], 0)
+        i += 1
+        if depth == 0:
+            return i
+
+
+def test_all_ctas_of_a_cluster_reach_both_of_its_barriers():
+    """The cluster form of kv_attention_kernel meets twice: when its parts are there, and when all have read them.  A CTA that left
+    before would keep the others waiting, without a limit."""
+    for name, body in KERNELS.items():
+        assert body.count("cluster_sync()") == (2 if name == "kv_attention_kernel" else 0), name
+    code = CODE["baps_kv_attention.cuh"]
+    assert code.count("barrier.cluster.arrive") == code.count("barrier.cluster.wait") == 1          # both in cluster_sync itself
+    assert sum(CODE[n].count("barrier.cluster") for n in NEW) == 2
+    body = KERNELS["kv_attention_kernel"]
+    # what the cluster form runs of it: without the other form's branch, and without the bodies of lambdas, whose returns are their own
+    first = body.index("if constexpr (kClusters) {")
+    other = block_end(body, first)
+    assert body[other:].lstrip().startswith("else {")
+    path = body[:other] + body[block_end(body, other):]
+    while "[&]" in path:
+        at = path.index("[&]")
+        path = path[:at] + path[block_end(path, at):]
+    ahead = path[:path.rindex("cluster_sync()")]
+    assert "return" not in ahead and "break" not in ahead and "kClusters || w < w1;" in ahead
+    # both barriers stand in the one block of the cluster form, at its top level, and the block ends with the kernel
+    at = path.rindex("if constexpr (kClusters) {")
+    block = path[at:block_end(path, at)]
+    depth = 0
+    depths = []
+    for i, c in enumerate(block):
+        depth += {"{": 1, "}": -1}.get(c, 0)
+        if block.startswith("cluster_sync()", i):
+            depths.append(depth)
+    assert depths == [1, 1] and re.search(r"cluster_sync\(\);\s*return;\s*}$", block)
