@@ -86,9 +86,8 @@ def test_all_ctas_of_a_cluster_reach_both_of_its_barriers():
     other = block_end(body, first)
     assert body[other:].lstrip().startswith("else {")
     path = body[:other] + body[block_end(body, other):]
-    while "[&]" in path:
-        at = path.index("[&]")
-        path = path[:at] + path[block_end(path, at):]
+    while (at := re.search(r"= \[&?\]", path)) is not None:
+        path = path[:at.start()] + path[block_end(path, at.start()):]
     ahead = path[:path.rindex("cluster_sync()")]
     assert "return" not in ahead and "break" not in ahead and "kClusters || w < w1;" in ahead
     # both barriers stand in the one block of the cluster form, at its top level, and the block ends with the kernel
