@@ -260,8 +260,9 @@ typedef struct {
  * sequence; where it grew, all codes of that page and head that the call does not write -- places behind the new tokens
  * included -- are rounded again: code = E4M3(value(code) * old / new).  A new element becomes E4M3(x / s), to
  * nearest even, infinities to +-448, NaN to NaN.  A page whose first place is written begins anew.
- * Two sequences must not write to one page in the same call.  Codes and scales do not depend on how tokens are spread
- * over calls, but for the second rounding of elements that a grown scale makes subnormal.
+ * No two entries of the table that a call writes through may name the same page.  Codes and scales do not depend on how tokens are
+ * spread over calls, but for the second rounding of elements that a grown scale makes subnormal, and for infinities, which
+ * become 448 times the scale of their call and, like any element, are rounded again when it grows.
  * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16.  Supported: B <= 65535; 2 * Hkv * (pages that max_new tokens touch) < 2^31.  */
 baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const void *v_new, const int64_t *strides,
                            int64_t n_tokens, const int32_t *starts, const int32_t *lengths, const int32_t *table,

@@ -151,3 +151,24 @@ def test_refusals():
     with pytest.raises(binding.BapsError) as e:
         binding.baps_kv_append(cache, shifted, shifted, table, lengths, starts)
     assert e.value.status == -3
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_an_infinity_is_448_of_its_calls_scale_and_shrinks_when_that_grows(dtype):
+    """In one call with the token behind it, or in a call of its own: not the same values, each the definition's."""
+    x = torch.ones(2, 1, 64)
+    x[0, 0, :2] = torch.tensor([float("inf"), float("-inf")])
+    x[1] = 4096.0
+    x = x.to(dtype).cuda()
+    table, zero = torch.tensor([[1]], dtype=torch.int32), torch.tensor([0], dtype=torch.int32)
+    got = []
+    for calls in ([(0, 2)], [(0, 1), (1, 2)]):
+        state = pool(2, 1, 16, 64, 2)
+        ref = serving.Cache(*state)
+        for a, b in calls:
+            at = zero + a, torch.tensor([0, b - a], dtype=torch.int32)
+            run(state, (x[a:b], x[a:b]), table, *at)
+            ref.append((x[a:b], x[a:b]), table, *at)
+            check(state, ref)
+        got.append(float(ref.value[0][1, 0, 0, 0] * ref.scale[0][1, 0]))
+    assert got == [448 * 16.0, 448 * 2.0 ** -8]                  # scales of 4096 (2^4) and of 1 (2^-8)
