@@ -214,7 +214,10 @@ baps_status baps_attention_restart_rates_static(const void *q, const void *k, co
  *
  * The calls below serve one decoding loop: baps_attention_window_fwd the prompts, baps_kv_append the keys and
  * values that go into the cache, baps_kv_attention the new tokens, baps_kv_fork and baps_kv_compact the pages.
- * They compute the plain softmax (Eq. (1)), in single precision around tensor-core products; none of Algorithm 1.
+ * They compute the plain softmax (Eq. (1)), none of Algorithm 1: scores, maxima, sums and outputs in single precision; the
+ * products run on tensor cores, so that each weight is rounded to their operands' type -- that of the inputs in
+ * baps_attention_window_fwd (half a step, 2^-8 of a bf16 or 2^-11 of an fp16 weight), fp16 in baps_kv_attention, which also scales bf16
+ * queries to fp16 (what is lost is below 2^-25 of a row's largest element) -- after the weights have been summed.
  *
  * Visibility.  The query at position p sees key j where j <= p and (j > p - window or j < sinks): itself, the
  * window - 1 keys before it and the sequence's first `sinks` keys.  window >= 1 (INT32_MAX: all), sinks >= 0.
@@ -228,6 +231,8 @@ baps_status baps_attention_restart_rates_static(const void *q, const void *k, co
  * q, k and v does not matter.  lse: NULL or device float [B, H, S], the natural logarithm of the sum of exponentials.
  * strides: NULL for contiguous [B, heads, S, D], else 12 int64 in elements: batch, head and row of q, k, v and out,
  * each at least 8 and a multiple of 8; the D elements of a row are contiguous.  Tensors must not overlap out.
+ * Weights of up to 2^8 times values are summed in single precision and then divided: 2^8 * (keys that a row sees) * |v| has to
+ * stay below 2^128 (bf16 values beyond about 1e31 can come out infinite).
  * dtype: BAPS_DTYPE_BF16 or BAPS_DTYPE_F16 (q, k, v and out).  scale: 0 selects 1/sqrt(D), at most 2^127.
  * Supported (else BAPS_ERR_UNSUPPORTED): D in {64, 128}; 1 <= S <= 2^31 - 256; H % Hkv == 0; B, H <= 65535;
  * B * H * (query tiles of 128 rows) < 2^31.                                                                */
@@ -237,7 +242,8 @@ baps_status baps_attention_window_fwd(const void *q, const void *k, const void *
 
 /* ---- The cache ---------------------------------------------------------------------------------------
  * A pool of pages.  k, v: [n_pages, Hkv, page, D] FP8 E4M3 codes (OCP, as in baps_attention_fwd_fp8); k_scale, v_scale:
- * [n_pages, Hkv] float32, one power of two per page and head: an element stands for value(code) * scale.  All device memory of
+ * [n_pages, Hkv] float32, one power of two from 2^-126 to 2^126 per page and head (baps_kv_append writes 2^-108 to 2^120): an
+ * element stands for value(code) * scale.  All device memory of
  * the caller, codes 16-byte and scales 4-byte aligned.  Supported by every call (else BAPS_ERR_UNSUPPORTED): page in
  * {16, 32, 64, 128}, D in {64, 128}, Hkv <= 32767, n_pages * Hkv * page < 2^31.
  * A sequence's pages are named by its row of a table, int32 [rows, table_width]: token j stands at place j % page of page
@@ -271,7 +277,8 @@ baps_status baps_kv_append(const baps_kv_cache *cache, const void *k_new, const 
 /* ---- Attention of the last T tokens of every sequence over the cache ------------------------------------
  * q, out: [B, H, T, D]; query t of sequence b stands at position lengths[b] - T + t, keys are those of positions
  * 0 .. lengths[b] - 1 (lengths: device int32 [B], the new tokens included; read as limited to 0 .. table_width * page).
- * A row that sees no key (a position below 0, pages that are not there) gives zeros and an lse of -infinity.
+ * A row that sees no key (a position below 0, pages that are not there) gives zeros and an lse of -infinity.  q and the cache must
+ * not overlap out.
  * Only pages that hold a visible key are read.  lse: NULL or device float [B, H, T].  strides: NULL for contiguous, else
  * 6 int64 in elements, multiples of 8: batch, head and token of q, then of out.
  * workspace: device memory, 16-byte aligned, at least baps_kv_attention_workspace() bytes (NULL if those are 0), contents
@@ -294,13 +301,16 @@ size_t baps_kv_attention_workspace(int B, int H, int Hkv, int T, int D, int page
  * continuation of old row parents[i] -- forked where a parent is named several times, moved where once, its pages given up
  * where never, an empty row (length 0) where parents[i] is outside 0 .. rows - 1 -- with room for `reserve` more tokens.
  *   - Full pages are shared.  The page that a sequence ends in (length % page != 0) goes to the parent's first child;
- *     every further child gets a copy of it in a free page.
+ *     every further child gets a copy of it in a free page.  So it has to stand in one row of the old table only: a length that
+ *     is set back into a page which other rows share gives a page that several rows would write to (refs is not asked).
  *   - Pages whose keys no later query sees (window, sinks as above, the next query at position length) are let go: -1.
  *   - Behind them come free pages for tokens up to length + reserve.
  *   - Free pages are those with refs == 0, taken lowest first, row after row (a row's copy before its reserve).  The
  *     first row that finds too few, and every row behind it, gets length -1 and no pages; so does a row that
  *     table_width cannot hold (which takes none from the rows behind it).
- *   - new_refs[p]: number of entries of new_table that name page p.  new_table is -1 elsewhere.
+ *   - new_refs[p]: number of entries of new_table that name page p.  new_table is -1 elsewhere.  Pages that something outside this
+ *     table holds, and pages reserved before for tokens that have not come, are free in new_refs.
+ *   - A length below 0 counts as 0: children of a row that had found no room begin empty.
  * refs (16-byte aligned, the other arrays 4-byte), new_refs: device int32 [cache->n_pages]; table [rows, table_width], new_table [new_rows, table_width]; lengths [rows],
  * new_lengths [new_rows].  In- and outputs must not overlap.  workspace: at least baps_kv_pages_workspace(new_rows, n_pages)
  * bytes, 16-byte aligned.  cache->k and v are only written for copies.

@@ -4,7 +4,7 @@
 //     m = running maximum, l = sum 2^(c s - m), O~ = sum 2^(c s - m) v;   O = O~ / l, lse = ln 2 (m + log2 l)
 // with s = q . k and c = log2(e) * scale.  m is held back: it moves only when a row's maximum passes it by more than 8
 // (weights stay below 2^8, exact in what follows), so that O~, which lives in tensor memory, is hardly ever rescaled.
-// S, l and O~ are float32; the weights are rounded to the inputs' type for the P V product (half a step, 2^-9 or 2^-12
+// S, l and O~ are float32; the weights are rounded to the inputs' type for the P V product (half a step, 2^-8 or 2^-11
 // of each weight) and summed before that rounding.
 //
 // Heads of 128: one CTA owns two consecutive 128-row query tiles (t = 0, 1; small grids: one) of one head, which share the K / V
@@ -29,6 +29,7 @@
 // Heads of 64: a padded batch of 8 x 4001 tokens, 16 / 4 heads, window 500, 20 first tokens: 117 us; as two streams per CTA, one CTA per SM 169 (a CTA
 // lives for six or seven tiles: its start and end are as long as its work), one stream and 128-key tiles, two per SM 134. Chunks of 32 keys that
 // no row of a warp sees are skipped (144 to 134 us).
+// 96 registers at launch: the form with two query tiles spills 8 bytes, the one with heads of 64 36.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -444,6 +445,10 @@ static inline baps_status window_launch(const CUtensorMap *maps, WindowParams &p
 }
 
 // Two query tiles per CTA share their K / V stream; one where that leaves SMs without a CTA.
+// Measured, us, one / two tiles per CTA (heads x tokens, window).  Fewer pairs of tiles than SMs, where one is taken: 37 x 333, 128: 8.4, 9.5; 28 x 1024,
+// all: 18.3, 21.0; 9 x 2048, 512: 13.3, 18.3; 3 x 8192, 4096: 55, 71.  As many and more, two: 37 x 1024, all: 21.7, 21.2; 18 x 2048, 512: 25.4, 18.9; 5 x
+// 8192, 4096: 107, 71; but 95 x 333, 128: 14.2, 18.2.  Short of the line, where single tiles of even length come to a second wave, the rule
+// is behind: 14 x 2048, 512: 25.0, 18.8; 3 x 8192, 1000: 37, 27.
 static inline int window_box_keys(int D) { return D == 64 ? 64 : 128; }
 template <typename T16>
 static inline baps_status window_shape(const CUtensorMap *maps, WindowParams &p, int D, cudaStream_t stream)

@@ -9,7 +9,8 @@
 // scale) for single tokens.  A group of warps owns one page and head of K or of V, keeps what it has read in registers
 // between the maximum and the conversion, and so reads its tokens once.  A thread holds eight times 16 bytes at most and the
 // kernel is held to 64 registers, so that an SM has 1024 threads' loads in flight (128 KB): 12 prompts of up to 8K tokens, 8 heads of
-// 128, pages of 64: 84 us (5.9 TB/s), 93 us with 91 registers and 640 threads.
+// 128, pages of 64: 84 us (5.9 TB/s), 93 us with 91 registers and 640 threads.  The forms in which a thread holds eight loads, this one among them, spill
+// 44 bytes, or 72 where one warp has a page to itself (16 tokens of 128, 32 of 64); the others nothing.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -175,7 +176,9 @@ static inline baps_status kv_append_launch(const KvAppendParams &p, cudaStream_t
     if (blocks > 0x7fffffffLL) return BAPS_ERR_UNSUPPORTED;
     return launch_kernel(kv_append_kernel<T16, D, kPage, kRowsMost>, dim3((unsigned)blocks, 1, (unsigned)p.B), A::kThreads, 0, stream, p);
 }
-// Few tokens per sequence: a page gets no more rows than that, and fewer threads read them (96 sequences, one token: 2.6 us).
+// Few tokens per sequence: a page gets no more rows than that, and fewer threads read them.  Measured, us, few / whole pages: 96 sequences, 8 heads of
+// 128, pages of 64: one token 2.8, 5.7, eight 3.1, 7.0; pages of 16: 2.8, 3.2 and 3.1, 4.4; 8 sequences 1.7, 2.4 and 1.8, 3.0.  (A third form for up
+// to 16 tokens would gain too: 16 of them 4.6 for 7.3.)
 template <typename T16, int D, int kPage>
 static inline baps_status kv_append_rows(const KvAppendParams &p, cudaStream_t stream)
 {

@@ -6,13 +6,14 @@
 // with c = log2(e) * scale and a running reference m, six below a maximum that is followed when a score passes it by more
 // than 8, so that weights stay below 2^14.  Codes become fp16 in registers (exactly: E4M3 has 4 significant bits), q is scaled
 // by a power of two per row so that its 8 or 11 bits fit fp16 (what is lost is below 2^-25 of the row's largest element),
-// and both products run on mma.sync m16n8k16 with float32 accumulation; the weights are rounded to fp16 (half a step, 2^-12)
+// and both products run on mma.sync m16n8k16 with float32 accumulation; the weights are rounded to fp16 (half a step, 2^-11)
 // after they have been summed.  The scales are applied in float32; O~ is kept in units of a value scale that is followed
 // where a page's leaves [unit / 64, unit], down to 2^-64 of the largest that there was: O~, below 2^14 * 448 in units of that one
 // for each key, then stays below 2^118 for 2^31 keys, and what is smaller does not count.
 //
 // What bounds it: the bytes of K and V, one per element: 48 sequences of 8192 to 32768 tokens, 32 / 8 heads of 128, pages of 64,
-// 298 us, 6.7 TB/s.  mma.sync, not tcgen05: the codes have to be widened in registers on the way, and a CTA has 8 to 32 rows of
+// 298 us for one draw of lengths (2.00 GB) ten times in a graph, 6.7 TB/s, some of it from L2; 316 us with lengths and pages drawn anew for each
+// call (2.01 GB on average), 6.4 TB/s.  mma.sync, not tcgen05: the codes have to be widened in registers on the way, and a CTA has 8 to 32 rows of
 // queries, where a tcgen05 tile has 128.  K and V are the operand with 16 rows and the queries the one with 8 columns
 // (S^T = K Q^T, O^T = V^T P^T), so that eight query rows waste nothing: a product of 16 x 8 x 16 takes 8 cycles of a scheduler's
 // tensor core and covers 256 codes.  (Queries as the 16 rows: twice the products, 471 us.  E4M3 operands, q and weights in two
@@ -760,9 +761,14 @@ kv_join_kernel(const KvAttnParams p)
 // as many as still run all at the same time, or to one CTA: one launch, nothing to join through memory, no CTA with two items.
 // That is taken where a CTA gets few enough tiles for it (most_tiles: what an item can have, by the table's width and the window):
 //   24 for an item to itself, 16 in a cluster, 36 where the window sets the length and the clusters fill four fifths of the machine.
-// Measured against the even cut, us (clusters first; 32 / 8 heads of 128 unless said): one sequence of 2000 tokens 7.1, 10.1; of 8000 12.7, 14.0; of
-// 12000 (24 tiles) 15.0, 12.7; six of up to 8000 (21 tiles, lengths differ) 22.3, 18.2; 30 of 1500 (a CTA each) 16.5, 21.8; 60 of 1500 32.2, 38.8;
-// 32 with window 4096, four queries each: 16 / 4 heads of 64 20.7, 26.1; of 128 32.6, 39.0.
+// Measured against the even cut, us (clusters first, 32 / 8 heads of 128, lengths from a quarter of the longest unless said):
+//   an item to itself: 30 sequences of up to 1536 tokens (24 tiles) 16.8, 22.2, 75 of them 37.2, 47.1; beyond the line still, 30 of 2048 21.5, 26.0, of
+//   3000 29.5, 30.3;
+//   clusters of eight: one sequence of 2000 6.5, 10.1, of 4000 8.2, 11.2, of 8192 (16 tiles) 11.2, 10.1; two of 8192 12.5, 14.2, four 13.2, 16.2; beyond,
+//   one of 12000 14.3, 13.0, of 16000 17.8, 14.5, four of 12000 17.0, 17.5;
+//   where a window of 4096 sets the length, 16 / 4 heads: 32 sequences (clusters of two, 35 tiles) 27.3, 32.3, 37 of them 29.8, 35.5; 20 (of three) 16.7, 21.1; 16 (of
+//   four) 14.3, 18.9; four queries each and heads of 64 (of three) 20.2, 25.9; short of the line, 25 sequences (200 of 296 places) 23.3, 25.2; beyond,
+//   window 5000 31.5, 36.3.  So the lines are on the even cut's side by up to a fifth, but for one sequence alone, which loses a tenth at 8192.
 struct KvShape { int tiles, groups, ctas, cluster; };
 static inline KvShape kv_shape(int R, int D, int64_t items, int64_t most_tiles, bool by_window)
 {

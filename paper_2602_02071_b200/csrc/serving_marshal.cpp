@@ -4,7 +4,7 @@
 // What a call has to do on the host before its kernels start -- check the tensors' types, shapes, strides and device,
 // allocate the outputs, pass pointers to the C ABI of include/baps.h, raise on a status -- and nothing else.  Kernels of the
 // smallest calls take 3 to 10 us, so the host is what bounds them: one token appended took 12.7 us with these steps in Python,
-// 8.8 with torch's Python methods called from C, 5.1 as here; a fork of beams 21.8, 18.1 and 10.5.  The library's functions
+// 8.8 with torch's Python methods called from C, 5.6 as here; a fork of beams 21.8, 18.1 and 11.5.  The library's functions
 // come as addresses (bind), so that there is one loaded library, that of binding.load().
 //
 // The interpreter's lock is let go before anything is allocated or launched: torch's allocator may wait for other threads.
