@@ -390,13 +390,17 @@ class KvCache:
         (_serving or _marshal()).fill_cache(self, k, v, k_scale, v_scale)         # struct: bytes of a baps_kv_cache, device
 
     def __setattr__(self, name, value):
-        raise AttributeError(f"KvCache.{name} cannot be assigned: make a new KvCache")
+        if name in KvCache.__slots__:
+            raise AttributeError(f"KvCache.{name} cannot be assigned: make a new KvCache")
+        object.__setattr__(self, name, value)    # (of a derived class)
 
     def __delattr__(self, name):
-        raise AttributeError(f"KvCache.{name} cannot be deleted")
+        if name in KvCache.__slots__:
+            raise AttributeError(f"KvCache.{name} cannot be deleted")
+        object.__delattr__(self, name)
 
     def __reduce__(self):                        # copies and pickles are made of their own tensors
-        return KvCache, (self.k, self.v, self.k_scale, self.v_scale)
+        return type(self), (self.k, self.v, self.k_scale, self.v_scale)
 
     @classmethod
     def empty(cls, n_pages: int, Hkv: int, page: int, D: int, device="cuda") -> "KvCache":

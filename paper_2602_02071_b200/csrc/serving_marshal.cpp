@@ -139,8 +139,9 @@ float real(PyObject* o)
 // The struct of a KvCache and its device, which has to be the current one.
 struct Cache {
     baps_kv_cache c;
-    int device;
+    int device, zero;                              // (no bytes that are nobody's: structs are compared as memory)
 };
+static_assert(sizeof(Cache) == sizeof(baps_kv_cache) + 2 * sizeof(int) && sizeof(baps_kv_cache) == 4 * sizeof(void*) + 4 * sizeof(int), "no padding");
 // The struct of a KvCache's tensors.
 Cache cache_of_tensors(PyObject* const* a)
 {
@@ -148,8 +149,8 @@ Cache cache_of_tensors(PyObject* const* a)
     const Sizes s = k.sizes();
     if (s.size() != 4 || !k.is_cuda()) refuse("k", "CUDA codes [n_pages,Hkv,page,D]");
     Cache cache;
-    std::memset(&cache, 0, sizeof(cache));         // padding too
     cache.device = k.get_device();
+    cache.zero = 0;
     cache.c.k = static_cast<decltype(cache.c.k)>(buffer(a[0], "k", kByte, s, cache.device));
     cache.c.v = static_cast<decltype(cache.c.v)>(buffer(a[1], "v", kByte, s, cache.device));
     cache.c.k_scale = static_cast<float*>(buffer(a[2], "k_scale", kFloat, s.slice(0, 2), cache.device));

@@ -225,3 +225,20 @@ def test_copies_of_a_cache_are_caches_of_their_own_tensors():
         binding.baps_kv_append(c, new, new, table, lengths - 1, starts)
         assert not torch.equal(c.k, before[0])
     assert all(torch.equal(a, b) for a, b in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), before))
+
+
+class Named(binding.KvCache):
+    """A class of a user's, with a member of its own."""
+
+
+@pytest.mark.gpu
+def test_a_derived_cache_keeps_its_class_and_its_own_members():
+    cache, q, table, lengths, _ = made()
+    named = Named(cache.k, cache.v, cache.k_scale, cache.v_scale)
+    named.name = "a"
+    named.name = "b"
+    del named.name
+    with pytest.raises(AttributeError):
+        named.k = cache.k
+    assert type(copy.copy(named)) is Named and type(pickle.loads(pickle.dumps(named))) is Named
+    assert torch.equal(binding.baps_kv_attention(q, named, table, lengths), binding.baps_kv_attention(q, cache, table, lengths))
